@@ -14,6 +14,9 @@
  *   decompression       rebuild to the dense dimension and      Sec. III-A (t_decompress), Alg. 1 Aggregate
  *                       sum W workers' messages
  *
+ * and, around it, what a language model's training step needs next to the compressed gradient: the embedding's lookup and
+ * its gradient by token.
+ *
  * Conventions
  *   - "device pointer": memory of the current HIP device (any allocator).  "host pointer":
  *     ordinary host memory, read before the call returns.
@@ -78,6 +81,11 @@ extern "C" {
                                          workgroups of the exact route wait for one more than there are and give up after a
                                          few polls, so that the call ends with the internal-error flag of
                                          gravac_read_status set and with unspecified outputs */
+
+/* element types of the operators that take more than binary32 */
+#define GRAVAC_FLOAT32 0
+#define GRAVAC_BFLOAT16 1
+#define GRAVAC_FLOAT16 2
 
 /*
  * Number of pairs a call will emit for a tensor of n elements at compression factor cf:
@@ -301,6 +309,60 @@ int gravac_decompress_update(const int32_t* idx, const float* val,
 int gravac_decompress_accumulate_static(const int32_t* idx, const float* val,
                                         const int64_t* counts, int W,
                                         int64_t n, float* dense_out, void* stream);
+
+/*
+ * ---- The embedding of a language model beside its compressed gradient ----------------------------------------------
+ *
+ * The gradient that a language model's worker compresses (Table I trains one) begins with its embedding: the rows of the
+ * tokens in the batch hold the sums of their positions' gradients, all others are zero.  These calls are the two ends of
+ * that: the lookup of rows by token, and the table's gradient, written straight into the flat gradient that
+ * gravac_compress takes.  Both consist of kernel launches only and can be recorded into a graph.
+ *
+ * Common arguments
+ *   vocab, dim      rows of the table, 1 .. 2^31 - 1, and elements of a row, 1 .. GRAVAC_EMBEDDING_MAX_DIM.
+ *   ..._stride      elements from one row to the next, >= dim and <= 2^31 - 1.  What lies between rows is neither read nor
+ *                   written.
+ *   tokens          device, int32 (token_bytes 4) or int64 (8) [n_tokens], aligned to its size.
+ *   n_tokens        0 .. GRAVAC_EMBEDDING_MAX_TOKENS.
+ *   ..._type        GRAVAC_FLOAT32, GRAVAC_BFLOAT16 or GRAVAC_FLOAT16; buffers may start at any element of their type.
+ */
+#define GRAVAC_EMBEDDING_MAX_DIM (1 << 20)
+#define GRAVAC_EMBEDDING_MAX_TOKENS (1 << 30)
+#define GRAVAC_FLAG_ACCUMULATE 16u    /* gravac_embedding_gradient: add to the table's gradient */
+
+/*
+ * out[t] = scale * table[tokens[t]] for every position t: the product in binary32, then one rounding to out's type.  A
+ * token outside [0, vocab) (a padded place) gives a row of +0.
+ *
+ *   table           device, table_type[vocab][table_stride], read only.
+ *   out             device, out_type[n_tokens][out_stride]; must not overlap the table.
+ */
+int gravac_embedding_lookup(const void* table, int table_type, int64_t vocab, int64_t dim, int64_t table_stride,
+                            const void* tokens, int token_bytes, int64_t n_tokens, float scale,
+                            void* out, int out_type, int64_t out_stride, void* stream);
+
+/*
+ * Gradient of the lookup with respect to the table: for every row v
+ *     table_grad[v] = scale * (sum of grad_out[t] over the positions t with tokens[t] == v)
+ * and +0 for a row that no position names; with GRAVAC_FLAG_ACCUMULATE the product is added to what table_grad holds, and
+ * rows that no position names are not touched (so alpha as scale and the table itself as table_grad are the SGD step of
+ * gravac_decompress_update on it).  The sums are binary32 and added up in an order that depends on the sizes and the tokens
+ * alone, so the result does not depend on scheduling.  A row's sum, the product and the sum with the old value are each
+ * rounded.
+ *
+ *   grad_out        device, grad_type[n_tokens][grad_stride], read only.
+ *   padding_token   positions with this token take no part, and neither do tokens outside [0, vocab).  Any value outside
+ *                   [0, vocab), such as -1, if there is no such token.
+ *   table_grad      device, float[vocab][table_stride]; must not overlap grad_out.
+ *   workspace       device, 256-byte aligned, at least gravac_embedding_gradient_workspace_bytes(n_tokens, vocab, dim)
+ *                   bytes: 16 per token, and for calls of more than 128 tokens two rows of partial sums per 4 to 32 tokens.
+ *   flags           0 or GRAVAC_FLAG_ACCUMULATE.
+ */
+int gravac_embedding_gradient_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, size_t* bytes_out);
+int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tokens, int64_t dim, int64_t grad_stride,
+                              const void* tokens, int token_bytes, int64_t padding_token, float scale,
+                              float* table_grad, int64_t vocab, int64_t table_stride,
+                              void* workspace, size_t workspace_bytes, unsigned flags, void* stream);
 
 /*
  * Diagnostics of the last gravac_compress call that used `workspace`: synchronises `stream`

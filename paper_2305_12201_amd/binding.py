@@ -27,11 +27,18 @@ MAX_CF = 8
 FLAG_FORCE_FALLBACK = 1
 FLAG_NO_COMMIT = 2
 FLAG_STALL_FALLBACK = 8
+FLAG_ACCUMULATE = 16
+FLOAT32 = 0
+BFLOAT16 = 1
+FLOAT16 = 2
+EMBEDDING_MAX_DIM = 1 << 20
+EMBEDDING_MAX_TOKENS = 1 << 30
 
 EXPORTS = (
     "gravac_topk_count", "gravac_workspace_bytes", "gravac_compress", "gravac_compress_profiled", "gravac_randomk_compress", "gravac_threshold_compress", "gravac_recompress", "gravac_commit",
     "gravac_decompress_workspace_bytes", "gravac_decompress_accumulate", "gravac_decompress_accumulate_static",
     "gravac_decompress_update",
+    "gravac_embedding_lookup", "gravac_embedding_gradient_workspace_bytes", "gravac_embedding_gradient",
     "gravac_read_status", "gravac_strerror",
     "gravac_controller_create", "gravac_controller_destroy", "gravac_controller_candidates",
     "gravac_controller_decide", "gravac_controller_finish_iteration", "gravac_controller_throughput",
@@ -109,6 +116,13 @@ def lib() -> ctypes.CDLL:
         L.gravac_decompress_accumulate_static.argtypes = [vp, vp, vp, i32, i64, vp, vp]
         L.gravac_decompress_workspace_bytes.restype = i32
         L.gravac_decompress_workspace_bytes.argtypes = [i32, i64, ctypes.POINTER(ctypes.c_size_t)]
+        L.gravac_embedding_lookup.restype = i32
+        L.gravac_embedding_lookup.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, ctypes.c_float, vp, i32, i64, vp]
+        L.gravac_embedding_gradient_workspace_bytes.restype = i32
+        L.gravac_embedding_gradient_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(ctypes.c_size_t)]
+        L.gravac_embedding_gradient.restype = i32
+        L.gravac_embedding_gradient.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, ctypes.c_float, vp, i64, i64, vp,
+                                                ctypes.c_size_t, u32, vp]
         L.gravac_read_status.restype = i32
         L.gravac_read_status.argtypes = [vp, vp, vp]
         L.gravac_strerror.restype = ctypes.c_char_p
@@ -302,6 +316,91 @@ def gravac_decompress_accumulate_static(idx, val, counts, dense_out, *, stream=N
         cnt.size, dense_out.numel(), _dev_ptr(dense_out, torch.float32), _stream_handle(stream))
     if rc != OK:
         raise GravacError(rc, "gravac_decompress_accumulate_static")
+
+
+_TYPES = {torch.float32: FLOAT32, torch.bfloat16: BFLOAT16, torch.float16: FLOAT16}
+
+
+def _type_of(dtype) -> int:
+    if dtype not in _TYPES:
+        raise TypeError(f"expected float32, bfloat16 or float16, got {dtype}")
+    return _TYPES[dtype]
+
+
+def _check_device(*tensors) -> None:
+    """The library works on the current device: a tensor of another one is refused."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError(f"expected a tensor of the current device cuda:{here}, got {t.device}")
+
+
+def _rows(t, what: str):
+    """(pointer, stride) of a matrix whose rows are consecutive elements."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected a matrix whose rows are consecutive elements")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _tokens(t):
+    """(pointer, bytes per token, number of tokens) of the tokens, in the order of the rows they stand for."""
+    if t.dtype not in (torch.int32, torch.int64) or not t.is_contiguous():
+        raise ValueError("tokens: expected contiguous int32 or int64")
+    return t.data_ptr(), t.element_size(), t.numel()
+
+
+def _workspace(t):
+    if t is None:
+        return 0, 0
+    if not t.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def gravac_embedding_lookup(table, tokens, out, *, scale=1.0, stream=None) -> None:
+    """``gravac_embedding_lookup`` of the C ABI: ``out[t] = scale * table[tokens[t]]``, a row of zeros for a token
+    outside the table.  ``table`` and ``out`` are matrices of float32, bfloat16 or float16 whose rows may lie apart;
+    ``tokens`` is contiguous int32 or int64 of any shape with as many entries as ``out`` has rows."""
+    _check_device(table, tokens, out)
+    tp, ts = _rows(table, "table")
+    op, os_ = _rows(out, "out")
+    kp, kb, n = _tokens(tokens)
+    if out.shape[0] != n or out.shape[1] != table.shape[1]:
+        raise ValueError(f"out: expected {n} rows of {table.shape[1]}, got {tuple(out.shape)}")
+    rc = lib().gravac_embedding_lookup(tp, _type_of(table.dtype), table.shape[0], table.shape[1], ts, kp, kb, n,
+                                       float(scale), op, _type_of(out.dtype), os_, _stream_handle(stream))
+    if rc != OK:
+        raise GravacError(rc, "gravac_embedding_lookup")
+
+
+def gravac_embedding_gradient_workspace_bytes(n_tokens: int, vocab: int, dim: int) -> int:
+    out = ctypes.c_size_t(0)
+    rc = lib().gravac_embedding_gradient_workspace_bytes(int(n_tokens), int(vocab), int(dim), ctypes.byref(out))
+    if rc != OK:
+        raise GravacError(rc, "gravac_embedding_gradient_workspace_bytes")
+    return int(out.value)
+
+
+def gravac_embedding_gradient(grad_out, tokens, table_grad, *, scale=1.0, padding_token=-1, accumulate=False, workspace,
+                              stream=None) -> None:
+    """``gravac_embedding_gradient`` of the C ABI: row v of ``table_grad`` (float32) becomes ``scale`` times the sum of
+    the rows of ``grad_out`` (float32, bfloat16 or float16) whose token is v, zeros if there is none; with ``accumulate``
+    it is added to what is there.  ``workspace``: a uint8 device tensor of at least
+    ``gravac_embedding_gradient_workspace_bytes`` bytes."""
+    _check_device(grad_out, tokens, table_grad, workspace)
+    gp, gs = _rows(grad_out, "grad_out")
+    tp, ts = _rows(table_grad, "table_grad")
+    kp, kb, n = _tokens(tokens)
+    if table_grad.dtype != torch.float32:
+        raise TypeError(f"table_grad: expected float32, got {table_grad.dtype}")
+    if grad_out.shape[0] != n or grad_out.shape[1] != table_grad.shape[1]:
+        raise ValueError(f"grad_out: expected {n} rows of {table_grad.shape[1]}, got {tuple(grad_out.shape)}")
+    wp, wb = _workspace(workspace)
+    rc = lib().gravac_embedding_gradient(gp, _type_of(grad_out.dtype), n, grad_out.shape[1], gs, kp, kb,
+                                         int(padding_token), float(scale), tp, table_grad.shape[0], ts, wp, wb,
+                                         FLAG_ACCUMULATE if accumulate else 0, _stream_handle(stream))
+    if rc != OK:
+        raise GravacError(rc, "gravac_embedding_gradient")
 
 
 def gravac_read_status(workspace, stream=None) -> dict:

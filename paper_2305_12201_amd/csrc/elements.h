@@ -1,0 +1,77 @@
+// elements.h - element types of the operators that take more than binary32 (GRAVAC_FLOAT32, _BFLOAT16, _FLOAT16):
+// conversion to and from binary32, and 16-byte accesses that need no more than the element's own alignment (global memory
+// of gfx950 takes them at any byte).
+#ifndef GRAVAC_ELEMENTS_H
+#define GRAVAC_ELEMENTS_H
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "gravac.h"
+
+namespace elements {
+
+struct F32 { using word = uint32_t; static constexpr int SIZE = 4; };
+struct BF16 { using word = uint16_t; static constexpr int SIZE = 2; };
+struct F16 { using word = uint16_t; static constexpr int SIZE = 2; };
+
+inline bool known(int type) { return type == GRAVAC_FLOAT32 || type == GRAVAC_BFLOAT16 || type == GRAVAC_FLOAT16; }
+inline int size_of(int type) { return type == GRAVAC_FLOAT32 ? 4 : 2; }
+
+template <typename E> __device__ __forceinline__ float to_float(typename E::word w);
+template <> __device__ __forceinline__ float to_float<F32>(uint32_t w) { return __uint_as_float(w); }
+template <> __device__ __forceinline__ float to_float<BF16>(uint16_t w) { return __uint_as_float((uint32_t)w << 16); }
+template <> __device__ __forceinline__ float to_float<F16>(uint16_t w) { return (float)__builtin_bit_cast(_Float16, w); }
+
+// one rounding to nearest, ties to even (gfx950 converts to bfloat16 and to binary16 in hardware)
+template <typename E> __device__ __forceinline__ typename E::word from_float(float x);
+template <> __device__ __forceinline__ uint32_t from_float<F32>(float x) { return __float_as_uint(x); }
+template <> __device__ __forceinline__ uint16_t from_float<BF16>(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+template <> __device__ __forceinline__ uint16_t from_float<F16>(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+
+// N consecutive elements as one access, at the alignment of an element
+template <typename E, int N>
+struct __attribute__((packed, aligned(E::SIZE))) Pack {
+    typename E::word w[N];
+};
+
+template <typename E, int N>
+__device__ __forceinline__ void load(const typename E::word* p, float (&x)[N])
+{
+    Pack<E, N> v;
+    __builtin_memcpy(&v, (const Pack<E, N>*)p, sizeof(v));
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = to_float<E>(v.w[i]);
+}
+
+template <typename E, int N>
+__device__ __forceinline__ void store(typename E::word* p, const float (&x)[N])
+{
+    Pack<E, N> v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v.w[i] = from_float<E>(x[i]);
+    __builtin_memcpy((Pack<E, N>*)p, &v, sizeof(v));
+}
+
+// ... and the first `n` of them (the end of a row)
+template <typename E, int N>
+__device__ __forceinline__ void load_part(const typename E::word* p, int n, float (&x)[N])
+{
+    if (n >= N) { load<E, N>(p, x); return; }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = i < n ? to_float<E>(p[i]) : 0.0f;
+}
+
+template <typename E, int N>
+__device__ __forceinline__ void store_part(typename E::word* p, int n, const float (&x)[N])
+{
+    if (n >= N) { store<E, N>(p, x); return; }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < n) p[i] = from_float<E>(x[i]);
+}
+
+}  // namespace elements
+
+#endif
