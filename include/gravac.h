@@ -15,7 +15,7 @@
  *                       sum W workers' messages
  *
  * and, around it, what a language model's training step needs next to the compressed gradient: the embedding's lookup and
- * its gradient by token.
+ * its gradient by token, and the update of weight matrices along an orthogonalised momentum.
  *
  * Conventions
  *   - "device pointer": memory of the current HIP device (any allocator).  "host pointer":
@@ -363,6 +363,68 @@ int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tok
                               const void* tokens, int token_bytes, int64_t padding_token, float scale,
                               float* table_grad, int64_t vocab, int64_t table_stride,
                               void* workspace, size_t workspace_bytes, unsigned flags, void* stream);
+
+/*
+ * ---- The update along an orthogonalised momentum --------------------------------------------------------------------
+ *
+ * Another step in the place of w - eta * g~ of Alg. 1, for parameters that are matrices: the momentum of the aggregated
+ * gradient with its singular values made equal, by Newton-Schulz products.  A matrix U becomes O by
+ *     X = U / (||U||_F + eps),   steps times   X <- a X + b (X X^T) X + c (X X^T)^2 X,   O = X
+ * (for more rows than columns with X^T X from the right, which is the same), whose products run on the matrix cores.
+ *
+ *   matrices        host, int64[n_mat][4], 1 <= n_mat <= GRAVAC_MAX_MATRICES: offset of the first element in the flat
+ *                   vector, rows, columns, elements from one row to the next (>= columns).  Rows and columns 1 .. 2^20, the
+ *                   smaller of the two up to 2^15.  All lie inside [0, n), in any order, and no two share an element;
+ *                   everything else of the flat vectors (biases, embeddings) is neither read nor written.
+ *   n               elements of the flat vectors, 1 .. 2^40.
+ *   type            GRAVAC_FLOAT32, GRAVAC_BFLOAT16 or GRAVAC_FLOAT16: elements of in and out, or of the parameters.  The
+ *                   products are as exact as in binary32, except with GRAVAC_BFLOAT16: there their operands are rounded to
+ *                   11 bits, which loses less than the result's own rounding to 8 (singular values of one matrix that are
+ *                   thousands of times apart can lose more: a step multiplies the smallest by a, their rounding with them).
+ *   steps           1 .. GRAVAC_MAX_STEPS.
+ *   coefficients    host, double[steps][3]: a, b, c of each step; NULL for 3.4445, -4.7750, 2.0315 in all of them.  Refused
+ *                   where a step could take a singular value above 3.9, or |b s^2 + c s^4| above 15: from singular values in
+ *                   [0, 1] (the norm is at least the largest), as the steps' extrema say.
+ *   eps             >= 0 and finite.  A matrix of zeros gives zeros, also with eps = 0; one with a NaN or an infinity gives
+ *                   NaN in all of its elements and changes no other matrix.
+ *   workspace       device, 256-byte aligned, at least gravac_orthogonalize_workspace_bytes(matrices, n_mat, type) bytes:
+ *                   about 12 per element of the matrices (8 with GRAVAC_BFLOAT16), sides rounded up to whole tiles,
+ *                   and 8 (4) per element of a square of the smaller side.
+ *
+ * The calls consist of kernel launches only and can be recorded into a graph; the host tables are read at capture time.
+ */
+#define GRAVAC_MAX_MATRICES 1024
+#define GRAVAC_MAX_STEPS 32
+#define GRAVAC_FLAG_NESTEROV 32u      /* gravac_orthogonal_update: look ahead along the momentum */
+
+int gravac_orthogonalize_workspace_bytes(const int64_t* matrices, int n_mat, int type, size_t* bytes_out);
+
+/*
+ * out = O of the matrices of in.  Both are flat vectors of the same layout; out may be in itself, and must not overlap it
+ * otherwise.
+ */
+int gravac_orthogonalize(const void* in, void* out, int type, int64_t n, const int64_t* matrices, int n_mat,
+                         int steps, const double* coefficients, double eps,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One step of the matrices of a flat parameter vector, element-wise products and sums each rounded to binary32:
+ *     momentum = beta * momentum + grad
+ *     U        = momentum, or with GRAVAC_FLAG_NESTEROV grad + beta * momentum (the new one)
+ *     params   = keep * params + (alpha * scales[i]) * O(U)      for matrix i
+ * With alpha = -eta and keep = 1 - eta * decay this is the step of rate eta with decoupled weight decay.  grad is the dense
+ * aggregate that gravac_decompress_accumulate leaves; parameters that are no matrices take gravac_decompress_update.
+ *
+ *   grad            device, float[n], read only.
+ *   momentum        device, float[n], updated in place.
+ *   params          device, type[n], updated in place (the sum is rounded once to type).
+ *   scales          host, float[n_mat], or NULL for 1: the step of each matrix, such as 0.2 sqrt(max(rows, columns)).
+ *   flags           0 or GRAVAC_FLAG_NESTEROV.
+ */
+int gravac_orthogonal_update(const float* grad, float* momentum, void* params, int type, int64_t n,
+                             const int64_t* matrices, int n_mat, float beta, float keep, float alpha, const float* scales,
+                             int steps, const double* coefficients, double eps,
+                             void* workspace, size_t workspace_bytes, unsigned flags, void* stream);
 
 /*
  * Diagnostics of the last gravac_compress call that used `workspace`: synchronises `stream`

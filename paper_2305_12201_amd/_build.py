@@ -7,7 +7,7 @@ import subprocess
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 SOURCE = os.path.join(_PKG, "csrc", "gravac.hip")
-OPERATOR_SOURCES = [os.path.join(_PKG, "csrc", "embedding.hip")]   # the operators beside the compression
+OPERATOR_SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("embedding.hip", "orthogonal.hip")]   # the operators beside the compression
 HOST_SOURCES = [os.path.join(_PKG, "csrc", "controller.cpp")]   # host-only parts of the same library
 LIBRARY = os.path.join(_PKG, "libgravac.so")
 

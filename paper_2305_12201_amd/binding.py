@@ -28,17 +28,21 @@ FLAG_FORCE_FALLBACK = 1
 FLAG_NO_COMMIT = 2
 FLAG_STALL_FALLBACK = 8
 FLAG_ACCUMULATE = 16
+FLAG_NESTEROV = 32
 FLOAT32 = 0
 BFLOAT16 = 1
 FLOAT16 = 2
 EMBEDDING_MAX_DIM = 1 << 20
 EMBEDDING_MAX_TOKENS = 1 << 30
+MAX_MATRICES = 1024
+MAX_STEPS = 32
 
 EXPORTS = (
     "gravac_topk_count", "gravac_workspace_bytes", "gravac_compress", "gravac_compress_profiled", "gravac_randomk_compress", "gravac_threshold_compress", "gravac_recompress", "gravac_commit",
     "gravac_decompress_workspace_bytes", "gravac_decompress_accumulate", "gravac_decompress_accumulate_static",
     "gravac_decompress_update",
     "gravac_embedding_lookup", "gravac_embedding_gradient_workspace_bytes", "gravac_embedding_gradient",
+    "gravac_orthogonalize_workspace_bytes", "gravac_orthogonalize", "gravac_orthogonal_update",
     "gravac_read_status", "gravac_strerror",
     "gravac_controller_create", "gravac_controller_destroy", "gravac_controller_candidates",
     "gravac_controller_decide", "gravac_controller_finish_iteration", "gravac_controller_throughput",
@@ -123,6 +127,13 @@ def lib() -> ctypes.CDLL:
         L.gravac_embedding_gradient.restype = i32
         L.gravac_embedding_gradient.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, ctypes.c_float, vp, i64, i64, vp,
                                                 ctypes.c_size_t, u32, vp]
+        L.gravac_orthogonalize_workspace_bytes.restype = i32
+        L.gravac_orthogonalize_workspace_bytes.argtypes = [vp, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.gravac_orthogonalize.restype = i32
+        L.gravac_orthogonalize.argtypes = [vp, vp, i32, i64, vp, i32, i32, vp, dbl, vp, ctypes.c_size_t, vp]
+        L.gravac_orthogonal_update.restype = i32
+        L.gravac_orthogonal_update.argtypes = [vp, vp, vp, i32, i64, vp, i32, ctypes.c_float, ctypes.c_float, ctypes.c_float,
+                                               vp, i32, vp, dbl, vp, ctypes.c_size_t, u32, vp]
         L.gravac_read_status.restype = i32
         L.gravac_read_status.argtypes = [vp, vp, vp]
         L.gravac_strerror.restype = ctypes.c_char_p
@@ -403,6 +414,80 @@ def gravac_embedding_gradient(grad_out, tokens, table_grad, *, scale=1.0, paddin
         raise GravacError(rc, "gravac_embedding_gradient")
 
 
+def _matrices(matrices):
+    """int64[n_mat][4] of (offset, rows, columns) or (offset, rows, columns, stride)."""
+    if isinstance(matrices, np.ndarray) and matrices.dtype == np.int64 and matrices.ndim == 2 and matrices.shape[1] == 4:
+        return np.ascontiguousarray(matrices)
+    rows = [tuple(int(v) for v in m) for m in matrices]
+    if any(len(m) not in (3, 4) for m in rows):
+        raise ValueError("matrices: expected (offset, rows, columns) or (offset, rows, columns, stride) each")
+    return np.array([m if len(m) == 4 else (*m, m[2]) for m in rows], dtype=np.int64).reshape(-1, 4)
+
+
+def _coefficients(coefficients, steps: int):
+    """double[steps][3], or None for the library's: one triple for all steps, or one for each."""
+    if coefficients is None:
+        return None
+    c = np.asarray(coefficients, dtype=np.float64)
+    if c.shape == (3,):
+        c = np.broadcast_to(c, (steps, 3))
+    if c.shape != (steps, 3):
+        raise ValueError(f"coefficients: expected three numbers or {steps} times three, got shape {c.shape}")
+    return np.ascontiguousarray(c)
+
+
+def _host_ptr(a):
+    return None if a is None else a.ctypes.data_as(ctypes.c_void_p)
+
+
+def _flat(t, n: int, dtype, what: str) -> int:
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{what}: expected {n} contiguous elements of {dtype}, got {t.numel()} of {t.dtype}")
+    return t.data_ptr()
+
+
+def gravac_orthogonalize_workspace_bytes(matrices, dtype=torch.float32) -> int:
+    m = _matrices(matrices)
+    out = ctypes.c_size_t(0)
+    rc = lib().gravac_orthogonalize_workspace_bytes(_host_ptr(m), m.shape[0], _type_of(dtype), ctypes.byref(out))
+    if rc != OK:
+        raise GravacError(rc, "gravac_orthogonalize_workspace_bytes")
+    return int(out.value)
+
+
+def gravac_orthogonalize(x, out, matrices, *, steps=5, coefficients=None, eps=1e-7, workspace, stream=None) -> None:
+    """``gravac_orthogonalize`` of the C ABI: the matrices of the flat vector ``x``, orthogonalised, into ``out`` (which may
+    be ``x``).  ``matrices``: (offset, rows, columns[, stride]) each; ``coefficients``: (a, b, c) for all steps or for each."""
+    _check_device(x, out, workspace)
+    m, c = _matrices(matrices), _coefficients(coefficients, steps)
+    wp, wb = _workspace(workspace)
+    n = x.numel()
+    rc = lib().gravac_orthogonalize(_flat(x, n, x.dtype, "x"), _flat(out, n, x.dtype, "out"), _type_of(x.dtype), n, _host_ptr(m),
+                                    m.shape[0], int(steps), _host_ptr(c), float(eps), wp, wb, _stream_handle(stream))
+    if rc != OK:
+        raise GravacError(rc, "gravac_orthogonalize")
+
+
+def gravac_orthogonal_update(grad, momentum, params, matrices, *, beta, alpha, keep=1.0, nesterov=False, scales=None, steps=5,
+                             coefficients=None, eps=1e-7, workspace, stream=None) -> None:
+    """``gravac_orthogonal_update`` of the C ABI: ``momentum = beta * momentum + grad`` (both float32), then
+    ``params = keep * params + alpha * scales[i] * O`` for matrix i, O the orthogonalised momentum (with ``nesterov``:
+    ``grad + beta * momentum``).  Arguments as for ``gravac_orthogonalize``."""
+    _check_device(grad, momentum, params, workspace)
+    m, c = _matrices(matrices), _coefficients(coefficients, steps)
+    s = None if scales is None else np.ascontiguousarray(np.asarray(scales, dtype=np.float32))
+    if s is not None and s.shape != (m.shape[0],):
+        raise ValueError(f"scales: expected {m.shape[0]} numbers, got shape {s.shape}")
+    wp, wb = _workspace(workspace)
+    n = params.numel()
+    rc = lib().gravac_orthogonal_update(
+        _flat(grad, n, torch.float32, "grad"), _flat(momentum, n, torch.float32, "momentum"), _flat(params, n, params.dtype, "params"),
+        _type_of(params.dtype), n, _host_ptr(m), m.shape[0], float(beta), float(keep), float(alpha), _host_ptr(s), int(steps),
+        _host_ptr(c), float(eps), wp, wb, FLAG_NESTEROV if nesterov else 0, _stream_handle(stream))
+    if rc != OK:
+        raise GravacError(rc, "gravac_orthogonal_update")
+
+
 def gravac_read_status(workspace, stream=None) -> dict:
     out = (ctypes.c_int32 * 8)()
     rc = lib().gravac_read_status(workspace.data_ptr(), _stream_handle(stream), out)
@@ -450,6 +535,41 @@ class Compressor:
 
     def status(self) -> dict:
         return gravac_read_status(self.workspace)
+
+
+class Orthogonalizer:
+    """Owns the workspace and the tables for repeated calls on the matrices of one flat vector."""
+
+    def __init__(self, n: int, matrices, dtype=torch.float32, steps: int = 5, coefficients=None, eps: float = 1e-7,
+                 device="cuda"):
+        self.n = int(n)
+        self.matrices = _matrices(matrices)
+        self.dtype = dtype
+        self.steps = int(steps)
+        self.coefficients = _coefficients(coefficients, self.steps)
+        self.eps = float(eps)
+        self.workspace = torch.empty(gravac_orthogonalize_workspace_bytes(self.matrices, dtype), dtype=torch.uint8,
+                                     device=device)
+
+    def _check(self, t):
+        if t.numel() != self.n or t.dtype != self.dtype:
+            raise ValueError(f"expected {self.n} elements of {self.dtype}, got {t.numel()} of {t.dtype}")
+
+    def __call__(self, x, out=None, stream=None):
+        """The matrices of ``x`` orthogonalised, into ``out`` or in place."""
+        self._check(x)
+        out = x if out is None else out
+        gravac_orthogonalize(x, out, self.matrices, steps=self.steps, coefficients=self.coefficients, eps=self.eps,
+                             workspace=self.workspace, stream=stream)
+        return out
+
+    def update(self, grad, momentum, params, *, beta, alpha, keep=1.0, nesterov=False, scales=None, stream=None):
+        """One step of the parameters' matrices along the orthogonalised momentum."""
+        self._check(params)
+        gravac_orthogonal_update(grad, momentum, params, self.matrices, beta=beta, alpha=alpha, keep=keep, nesterov=nesterov,
+                                 scales=scales, steps=self.steps, coefficients=self.coefficients, eps=self.eps,
+                                 workspace=self.workspace, stream=stream)
+        return params
 
 
 class Controller:

@@ -1,0 +1,344 @@
+"""Orthogonalised matrices and the update along them against the definition in 64 bits on the CPU."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2305_12201_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+QUINTIC = (3.4445, -4.7750, 2.0315)
+CUBIC = (1.5, -0.5, 0.0)
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+HALF_STEP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}   # relative, at most
+
+
+def _exact(G, steps=5, coefficients=QUINTIC, eps=1e-7, dtype=torch.float64):
+    a, b, c = coefficients
+    X = G.to(dtype)
+    X = X / (torch.linalg.vector_norm(G.double()).to(dtype) + eps)
+    if X.shape[0] > X.shape[1]:
+        X = X.t()
+    for _ in range(steps):
+        A = X @ X.t()
+        X = a * X + (b * A + c * (A @ A)) @ X
+    return X.t() if G.shape[0] > G.shape[1] else X
+
+
+def _rounded_operands(G, steps=5, coefficients=QUINTIC, eps=1e-7):
+    """The definition in 64 bits, except that the operands of the products are rounded to 11 bits (the diagonals of A and P
+    aside): what the calls on bfloat16 are specified to do."""
+    a, b, c = coefficients
+    r = lambda x, s: (x * s).to(torch.float16).double() / s  # noqa: E731
+    X = G.double()
+    X = X / (torch.linalg.vector_norm(X) + eps)
+    if X.shape[0] > X.shape[1]:
+        X = X.t()
+    m, n = X.shape
+    sx, sm = 2.0 ** min(14, round(math.log2(math.sqrt(m * n)))), 2.0 ** min(12, round(math.log2(m)))
+    for _ in range(steps):
+        H = r(X, sx)
+        A = H @ H.t()
+        d = A.diagonal().clone()
+        E = r(A - torch.diag(d), sm)
+        A2 = E @ E + (d[:, None] + d[None, :]) * E + torch.diag(d * d)
+        P = b * (E + torch.diag(d)) + c * A2
+        p = P.diagonal().clone()
+        X = (a + p)[:, None] * X + r(P - torch.diag(p), sm) @ H
+    return X.t() if G.shape[0] > G.shape[1] else X
+
+
+def _error(got, want):
+    return float(torch.linalg.vector_norm(got.double() - want) / torch.linalg.vector_norm(want))
+
+
+def _tolerance(G, dtype, steps=5, coefficients=QUINTIC, eps=1e-7):
+    """Relative to the norm of the result.
+
+    float32 and float16: a plain evaluation in binary32 rounds each operand and product by 2^-24.  Here an operand in two parts is off by
+    2^-22 at most, two of them and the dropped product of the low parts by 3 * 2^-22 = 12 * 2^-24 per product; sums are
+    binary32 either way.  So at most 12 times the error of the binary32 evaluation, no less than 2^-22 being asked for, and
+    the half step of the output's own rounding.
+    bfloat16: the error of rounded operands, which is a random walk through the same roundings (a different order of the
+    sums moves single ones): twice that, and the half step of the output's own rounding."""
+    want = _exact(G, steps, coefficients, eps)
+    if dtype != torch.bfloat16:
+        return 12 * _error(_exact(G, steps, coefficients, eps, torch.float32), want) + 2.0 ** -22 + \
+            (HALF_STEP[dtype] if dtype == torch.float16 else 0.0)
+    return 2 * _error(_rounded_operands(G, steps, coefficients, eps), want) + HALF_STEP[dtype]
+
+
+def _values(rows, cols, kind, seed):
+    g = torch.Generator().manual_seed(seed)
+    G = torch.randn(rows, cols, generator=g)
+    if kind == "low rank":
+        G = torch.randn(rows, 4, generator=g) @ torch.randn(4, cols, generator=g) + 0.1 * G
+    elif kind == "graded":
+        k = min(rows, cols)
+        U, _, V = torch.linalg.svd(G.double(), full_matrices=False)
+        G = (U @ torch.diag(10.0 ** (-4 * torch.arange(k).double() / k)) @ V).float()
+    return G
+
+
+def _orthogonalize(x, matrices, out=None, fill=0xA5, **kw):
+    """On a workspace of bytes that would be NaN."""
+    out = torch.empty_like(x) if out is None else out
+    ws = torch.full((B.gravac_orthogonalize_workspace_bytes(matrices, x.dtype),), fill, dtype=torch.uint8, device="cuda")
+    B.gravac_orthogonalize(x, out, matrices, workspace=ws, **kw)
+    return out
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (16, 16), (31, 33), (64, 147), (127, 129), (128, 128), (129, 128), (130, 390), (257, 300),
+          (300, 1100), (1025, 515), (3, 5000), (640, 640)]
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_orthogonalize(rows, cols, dtype):
+    for kind in ("normal", "low rank", "graded"):
+        G = _values(rows, cols, kind, rows * 31 + cols).to(dtype)
+        got = _orthogonalize(G.cuda().view(-1), [(0, rows, cols)], fill=255).cpu().view(rows, cols)
+        err, bound = _error(got, _exact(G)), _tolerance(G, dtype)
+        print(rows, cols, dtype, kind, "error %.2e of %.2e" % (err, bound))
+        assert err <= bound, kind
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("steps,coefficients", [(1, QUINTIC), (2, CUBIC), (12, CUBIC), (8, (15 / 8, -10 / 8, 3 / 8))])
+def test_other_steps_and_coefficients(dtype, steps, coefficients):
+    G = _values(96, 200, "normal", 5).to(dtype)
+    got = _orthogonalize(G.cuda().view(-1), [(0, 96, 200)], steps=steps, coefficients=coefficients).cpu().view(96, 200)
+    assert _error(got, _exact(G, steps, coefficients)) <= _tolerance(G, dtype, steps, coefficients)
+    if steps == 12:   # the cubic leads every singular value to 1
+        assert _error(got @ got.t().to(got.dtype), torch.eye(96).double()) <= 4 * _tolerance(G, dtype, steps, coefficients) + 1e-2
+
+
+def test_coefficients_of_each_step():
+    G = _values(70, 90, "normal", 6)
+    each = [(2.0, -1.5, 0.5), CUBIC, (1.0, 0.0, 0.0)]
+    got = _orthogonalize(G.cuda().view(-1), [(0, 70, 90)], steps=3, coefficients=each).cpu().view(70, 90)
+    X = G.double() / (torch.linalg.vector_norm(G.double()) + 1e-7)
+    for a, b, c in each:
+        A = X @ X.t()
+        X = a * X + (b * A + c * (A @ A)) @ X
+    assert _error(got, X) <= 3 * 12 * 2.0 ** -22      # three steps, each with 12 * 2^-24 per product and slopes below 2, times 4
+
+
+def test_a_vector_and_a_diagonal_in_closed_form():
+    a, b, c = QUINTIC
+    f = lambda s: a * s + b * s ** 3 + c * s ** 5  # noqa: E731
+    v = _values(1, 300, "normal", 7)
+    want = 1.0
+    for _ in range(5):
+        want = f(want)
+    got = _orthogonalize(v.cuda().view(-1), [(0, 1, 300)], eps=0.0).cpu().double()
+    assert _error(got, want * v[0].double() / torch.linalg.vector_norm(v.double())) <= 2.0 ** -19   # 311 (the slopes' product) 2^-24, twice that
+    d = torch.tensor([3.0, 4.0, 12.0, 84.0, 3612.0])       # of norm 3613
+    s = d.double() / 3613.0
+    for _ in range(5):
+        s = f(s)
+    got = _orthogonalize(torch.diag(d).cuda().view(-1), [(0, 5, 5)], eps=0.0).cpu().view(5, 5).double()
+    assert torch.equal(got - torch.diag(got.diagonal()), torch.zeros(5, 5).double())
+    assert ((got.diagonal() - s).abs() <= 2.0 ** -19 * s.abs().max()).all()
+
+
+def test_powers_of_two_and_transposes_change_no_bit():
+    G = _values(100, 260, "low rank", 8)
+    one = _orthogonalize(G.cuda().view(-1), [(0, 100, 260)], eps=0.0).cpu().view(100, 260)
+    for k in (-100, -40, 30, 100):
+        other = _orthogonalize((G * 2.0 ** k).cuda().view(-1), [(0, 100, 260)], eps=0.0).cpu().view(100, 260)
+        assert torch.equal(one, other), k
+    other = _orthogonalize(G.t().contiguous().cuda().view(-1), [(0, 260, 100)], eps=0.0).cpu().view(260, 100)
+    assert torch.equal(one, other.t())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_matrices_of_a_flat_vector(dtype):
+    """Every matrix of a call is what it is alone; what lies between them is left; in place as into another buffer."""
+    g = torch.Generator().manual_seed(9)
+    shapes = [(int(torch.randint(1, 150, (1,), generator=g)), int(torch.randint(1, 300, (1,), generator=g))) for _ in range(103)]
+    shapes += [(400, 130), (130, 700)]
+    at, matrices = 3, []
+    for r, c in shapes:
+        stride = c + (5 if len(matrices) % 4 == 1 else 0)
+        matrices.append((at, r, c, stride))
+        at += r * stride + len(matrices) % 3
+    # two matrices that share the rows of a larger one
+    matrices += [(at, 60, 20, 50), (at + 20, 60, 30, 50)]
+    at += 60 * 50 + 11
+    order = torch.randperm(len(matrices), generator=g).tolist()
+    x = torch.randn(at, generator=g).to(dtype)
+    inside = torch.zeros(at, dtype=torch.bool)
+    for o, r, c, s in matrices:
+        inside.as_strided((r, c), (s, 1), o).fill_(True)
+    got = _orthogonalize(x.cuda(), [matrices[i] for i in order], out=torch.full((at,), 7.0, dtype=dtype, device="cuda"))
+    assert (got.cpu()[~inside] == 7.0).all()
+    place = x.cuda()
+    _orthogonalize(place, matrices, out=place)
+    assert torch.equal(place.cpu()[~inside], x[~inside])
+    assert torch.equal(place.cpu()[inside], got.cpu()[inside])
+    for o, r, c, s in matrices[::9] + matrices[-4:]:
+        alone = _orthogonalize(x.as_strided((r, c), (s, 1), o).contiguous().cuda().view(-1), [(0, r, c)]).cpu()
+        assert torch.equal(alone.view(r, c), got.cpu().as_strided((r, c), (s, 1), o))
+
+
+def test_zeros_and_what_is_no_number():
+    shapes = [(40, 50), (40, 50), (50, 40), (20, 200), (40, 50)]
+    matrices = [(i * 4000, r, c) for i, (r, c) in enumerate(shapes)]
+    x = torch.randn(20_000, generator=torch.Generator().manual_seed(10))
+    x[:2000] = 0.0
+    x[4000 + 77], x[8000 + 5] = float("nan"), float("inf")
+    for eps in (0.0, 1e-7):
+        got = _orthogonalize(x.cuda(), matrices, eps=eps).cpu()
+        assert torch.equal(got[:2000], torch.zeros(2000))
+        assert torch.isnan(got[4000:6000]).all() and torch.isnan(got[8000:10_000]).all()
+        for i in (3, 4):
+            r, c = shapes[i]
+            G = x[i * 4000:i * 4000 + r * c].view(r, c)
+            assert _error(got[i * 4000:i * 4000 + r * c].view(r, c), _exact(G, eps=eps)) <= _tolerance(G, torch.float32, eps=eps)
+
+
+@pytest.mark.parametrize("size", [1e-38, 1e-30, 1e30, 3e37])
+def test_magnitudes(size):
+    G = _values(30, 70, "normal", 11) * size
+    got = _orthogonalize(G.cuda().view(-1), [(0, 30, 70)], eps=0.0).cpu().view(30, 70)
+    assert _error(got, _exact(G.double(), eps=0.0)) <= 12 * _error(_exact(G.double() / size, eps=0.0, dtype=torch.float32),
+                                                                 _exact(G.double() / size, eps=0.0)) + 2.0 ** -22
+
+
+def test_eps_stands_beside_the_norm():
+    G = _values(30, 70, "normal", 12) * 1e-9
+    got = _orthogonalize(G.cuda().view(-1), [(0, 30, 70)], eps=1e-7).cpu().view(30, 70)
+    assert _error(got, _exact(G, eps=1e-7)) <= _tolerance(G, torch.float32, eps=1e-7)
+
+
+# ---- update ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_update(dtype, nesterov):
+    shapes = [(64, 147), (200, 200), (300, 65), (1, 40)]
+    at, matrices = 5, []
+    for r, c in shapes:
+        matrices.append((at, r, c))
+        at += r * c + 17
+    g = torch.Generator().manual_seed(13)
+    grad, mom = torch.randn(at, generator=g) * 1e-3, torch.randn(at, generator=g) * 1e-2
+    params = (torch.randn(at, generator=g) * 0.02).to(dtype)
+    beta, keep, alpha = 0.95, 0.99, -0.02
+    f = lambda x: np.float32(x).item()  # noqa: E731
+    for scales in (None, [0.2 * max(r, c) ** 0.5 for r, c in shapes]):
+        dg, dm, dp = grad.cuda(), mom.cuda(), params.cuda()
+        o = B.Orthogonalizer(at, matrices, dtype)
+        o.update(dg, dm, dp, beta=beta, alpha=alpha, keep=keep, nesterov=nesterov, scales=scales)
+        # the momentum is two binary32 roundings, bit for bit; nothing else has changed outside the matrices
+        new = mom * f(beta) + grad
+        inside = torch.zeros(at, dtype=torch.bool)
+        for off, r, c in matrices:
+            inside[off:off + r * c] = True
+        assert torch.equal(dm.cpu(), torch.where(inside, new, mom))
+        assert torch.equal(dg.cpu(), grad) and torch.equal(dp.cpu()[~inside], params[~inside])
+        for i, (off, r, c) in enumerate(matrices):
+            part = slice(off, off + r * c)
+            U = (grad[part] + f(beta) * new[part] if nesterov else new[part]).view(r, c)
+            O = _exact(U)
+            step = f(alpha) * f(1.0 if scales is None else scales[i])
+            want = f(keep) * params[part].view(r, c).double() + step * O
+            err = torch.linalg.vector_norm(dp.cpu()[part].view(r, c).double() - want)
+            # the direction as in test_orthogonalize without its rounding to 16 bits; two binary32 roundings; one to the type
+            bound = abs(step) * (_tolerance(U, dtype) if dtype == torch.float32 else _tolerance(U, dtype) - HALF_STEP[dtype]) * torch.linalg.vector_norm(O)
+            bound = bound + (HALF_STEP[dtype] + 3 * 2.0 ** -24) * torch.linalg.vector_norm(want.abs() + params[part].view(r, c).double().abs())
+            assert err <= bound, (i, float(err), float(bound))
+
+
+def test_update_of_a_matrix_without_gradient():
+    n = 64 * 80
+    params = torch.randn(n, generator=torch.Generator().manual_seed(14)).cuda()
+    old = params.clone()
+    zero = torch.zeros(n, device="cuda")
+    B.Orthogonalizer(n, [(0, 64, 80)]).update(zero, zero.clone(), params, beta=0.9, alpha=-1.0, keep=0.5)
+    assert torch.equal(params, 0.5 * old)
+
+
+def test_several_steps_descend():
+    """ten steps on |W - V|^2 / 2 with the update against the same in 64 bits"""
+    r, c = 60, 110
+    V = _values(r, c, "normal", 15)
+    W, mom = torch.zeros(r * c, device="cuda"), torch.zeros(r * c, device="cuda")
+    w64, m64 = torch.zeros(r, c).double(), torch.zeros(r, c).double()
+    o = B.Orthogonalizer(r * c, [(0, r, c)])
+    dV = V.cuda().view(-1)
+    for _ in range(10):
+        grad = W - dV
+        o.update(grad, mom, W, beta=0.9, alpha=-0.1, nesterov=True)
+        g64 = w64 - V.double()
+        m64 = np.float32(0.9).item() * m64 + g64
+        w64 = w64 + np.float32(-0.1).item() * _exact(g64 + np.float32(0.9).item() * m64)
+    # ten directions, each off by at most 12 times the few 1e-7 of a binary32 evaluation, fed back through a slope of order one
+    assert _error(W.cpu().view(r, c), w64) <= 10 * 12 * 1e-6
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_captured_and_replayed_on_a_side_stream(dtype):
+    shapes = [(150, 330), (40, 20), (300, 128)]
+    at, matrices = 0, []
+    for r, c in shapes:
+        matrices.append((at, r, c))
+        at += r * c
+    g = torch.Generator().manual_seed(16)
+    o, e = B.Orthogonalizer(at, matrices, dtype), B.Orthogonalizer(at, matrices, dtype)
+    x, y = torch.zeros(at, dtype=dtype, device="cuda"), torch.zeros(at, dtype=dtype, device="cuda")
+    grad, mom, params = torch.zeros(at, device="cuda"), torch.zeros(at, device="cuda"), torch.zeros(at, dtype=dtype, device="cuda")
+
+    def calls(which):
+        which(x, y)
+        which.update(grad, mom, params, beta=0.9, alpha=-0.1, nesterov=True)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls(o)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(o)
+    for _ in range(4):
+        x.copy_(torch.randn(at, generator=g).to(dtype))
+        grad.copy_(torch.randn(at, generator=g))
+        m0, p0 = mom.clone(), params.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone(), mom.clone(), params.clone()
+        mom.copy_(m0), params.copy_(p0), y.zero_()
+        calls(e)
+        assert torch.equal(got[0], y) and torch.equal(got[1], mom) and torch.equal(got[2], params)
+        assert _error(y[:150 * 330].cpu().view(150, 330), _exact(x[:150 * 330].cpu().view(150, 330))) <= \
+            _tolerance(x[:150 * 330].cpu().view(150, 330), dtype)
+
+
+def test_binding_refuses():
+    x = torch.zeros(100, device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    table = [(0, 10, 10)]
+    with pytest.raises(ValueError):
+        B.gravac_orthogonalize(x.cpu(), x, table, workspace=ws)
+    with pytest.raises(ValueError):
+        B.gravac_orthogonalize(x, x[:50], table, workspace=ws)
+    with pytest.raises(ValueError):
+        B.gravac_orthogonalize(x, x.half(), table, workspace=ws)
+    with pytest.raises(TypeError):
+        B.gravac_orthogonalize(x.double(), x.double(), table, workspace=ws)
+    with pytest.raises(ValueError):
+        B.gravac_orthogonalize(x, x, table, coefficients=[(1, 0, 0)] * 3, workspace=ws)
+    with pytest.raises(ValueError):
+        B.gravac_orthogonal_update(x, x, x.clone(), table, beta=0.9, alpha=-0.1, scales=[1.0, 2.0], workspace=ws)
+    with pytest.raises(ValueError):
+        B.gravac_orthogonal_update(x, x.half(), x.clone(), table, beta=0.9, alpha=-0.1, workspace=ws)
+    with pytest.raises(B.GravacError) as e:
+        B.gravac_orthogonalize(x, x, table, workspace=ws[:1000])
+    assert e.value.code == B.ERR_WORKSPACE
+    with pytest.raises(ValueError):
+        B.Orthogonalizer(100, table)(torch.zeros(99, device="cuda"))
