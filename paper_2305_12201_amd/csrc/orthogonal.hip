@@ -37,13 +37,15 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-constexpr int T = 128;             // rows and columns of a tile
-constexpr int SLAB = 128;          // bytes of an operand's row that are in LDS at a time: 32 elements as hi and lo, or 64 hi
+constexpr int SLAB = 64;           // bytes of an operand's row that are fetched at a time: 16 elements as hi and lo, or 32 hi
+constexpr int BLOCK = 128;         // rows whose slabs stand together in memory
 constexpr int MAX_MAT = GRAVAC_MAX_MATRICES;
 constexpr int MAX_PARTS = 1024;    // partial sums of a matrix's norm at most
 constexpr int PART = 16384;        // elements of one
 constexpr int PER_INIT = 48;       // matrices of one launch of the table kernel (its argument holds them)
 constexpr int CUT = 64;            // side of a tile of the kernel that cuts a matrix into operands
+
+constexpr int LOW = 16;            // from a hi to its lo
 
 struct MatIn {   // what the host says of a matrix
     int64_t offset, stride, base;     // base: its part of the workspace
@@ -65,7 +67,7 @@ struct Mat {     // ... and what the kernels read
 
 struct Tile { uint32_t mat; uint16_t i, j; };
 
-__host__ __device__ inline int64_t padded(int64_t x) { return (x + T - 1) / T * T; }
+__host__ __device__ inline int64_t padded(int64_t x, int tile) { return (x + tile - 1) / tile * tile; }
 __host__ __device__ inline int64_t aligned(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
 // 2^round(log2(x)) up to 2^most
@@ -77,12 +79,12 @@ __host__ __device__ inline float power_of_two(double x, int most)
 }
 
 // Lays out a matrix's part of the workspace; returns its size.
-__host__ __device__ inline int64_t lay_out(Mat& d, int64_t rows, int64_t cols, int64_t base, bool split)
+__host__ __device__ inline int64_t lay_out(Mat& d, int64_t rows, int64_t cols, int64_t base, bool split, int tile)
 {
     d.rows = (int32_t)rows; d.cols = (int32_t)cols;
     d.tall = rows > cols;
     d.m = (int32_t)(d.tall ? cols : rows); d.n = (int32_t)(d.tall ? rows : cols);
-    d.mp = (int32_t)padded(d.m); d.np = (int32_t)padded(d.n);
+    d.mp = (int32_t)padded(d.m, tile); d.np = (int32_t)padded(d.n, tile);
     const int64_t el = split ? 4 : 2, xb = aligned(el * d.mp * d.np), ab = aligned(el * d.mp * d.mp);
     int64_t at = base;
     d.x = at; at += xb;
@@ -123,10 +125,38 @@ struct Call {
 // ---------------------------------------------------------------------------------------------------------------------
 
 struct InitArgs {
-    int32_t n, first, split;
+    int32_t n, first, split, tile;
     MatIn mat[PER_INIT];
 };
 static_assert(sizeof(InitArgs) + sizeof(Call) <= 4096 - 64, "kernel arguments");
+
+// Workgroups go to the eight dies (each with an L2 of its own) in turn.  Where tile number `at` of a matrix's `n` stands among
+// its n slots: each die gets a run of the list, whose tiles lie together in the matrix and share their operands' rows.
+// (`at` counted without regard to the dies: 4096 x 4096 in bfloat16 2.34 instead of 2.07 ms.)
+constexpr uint32_t DIES = 8;
+
+__device__ inline uint32_t slot_of(uint32_t at, uint32_t n)
+{
+    const uint32_t each = n / DIES, more = n % DIES, longer = more * (each + 1);   // `more` dies get one more than the others
+    if (at < longer) return at % (each + 1) * DIES + at / (each + 1);
+    return (at - longer) % each * DIES + more + (at - longer) / each;
+}
+
+// A matrix's tiles are listed in bands of BAND rows, column by column, so that a run is about as high as it is wide.
+constexpr uint32_t BAND = 8;
+
+__device__ inline uint32_t place_in_triangle(uint32_t r, uint32_t c, uint32_t n)   // c <= r < n
+{
+    const uint32_t k = r / BAND * BAND, h = n - k < BAND ? n - k : BAND, before = k * (k + 1) / 2;
+    if (c <= k) return before + c * h + (r - k);
+    const uint32_t q = c - k;   // columns behind the band's first row: h, h - 1, ... tiles each
+    return before + k * h + q * h - q * (q - 1) / 2 + (r - c);
+}
+__device__ inline uint32_t place_in_square(uint32_t r, uint32_t c, uint32_t rows, uint32_t cols)
+{
+    const uint32_t k = r / BAND * BAND, h = rows - k < BAND ? rows - k : BAND;
+    return k * cols + c * h + (r - k);
+}
 
 // One workgroup per matrix: its entry, and its lines in the tables of tiles and partial sums.
 __global__ __launch_bounds__(256) void table_kernel(Call p, InitArgs a)
@@ -134,20 +164,23 @@ __global__ __launch_bounds__(256) void table_kernel(Call p, InitArgs a)
     const MatIn& g = a.mat[blockIdx.x];
     const uint32_t id = (uint32_t)(a.first + blockIdx.x);
     Mat d;
-    lay_out(d, g.rows, g.cols, g.base, a.split != 0);
+    lay_out(d, g.rows, g.cols, g.base, a.split != 0, a.tile);
     d.offset = g.offset; d.stride = g.stride;
     d.cut = g.cut; d.part = g.part; d.parts = g.parts; d.scale = g.scale;
     if (threadIdx.x == 0) p.mats[id] = d;
-    const uint32_t tm = (uint32_t)d.mp / T, tn = (uint32_t)d.np / T;
+    const uint32_t tm = (uint32_t)(d.mp / a.tile), tn = (uint32_t)(d.np / a.tile);
     for (uint32_t i = threadIdx.x; i < tm * tm; i += 256) {
         const uint32_t r = i / tm, c = i % tm;
         if (c > r) continue;
         const Tile t = {id, (uint16_t)r, (uint16_t)c};
-        p.tiles[0][g.tile[0] + r * (r + 1) / 2 + c] = t;
-        p.tiles[1][g.tile[1] + r * (r + 1) / 2 + c] = t;
+        const uint32_t at = slot_of(place_in_triangle(r, c, tm), tm * (tm + 1) / 2);
+        p.tiles[0][g.tile[0] + at] = t;
+        p.tiles[1][g.tile[1] + at] = t;
     }
-    for (uint32_t i = threadIdx.x; i < tn * tm; i += 256)
-        p.tiles[2][g.tile[2] + i] = {id, (uint16_t)(i / tm), (uint16_t)(i % tm)};
+    for (uint32_t i = threadIdx.x; i < tn * tm; i += 256) {
+        const uint32_t r = i / tm, c = i % tm;
+        p.tiles[2][g.tile[2] + slot_of(place_in_square(r, c, tn, tm), tn * tm)] = {id, (uint16_t)r, (uint16_t)c};
+    }
     const uint32_t cuts = (uint32_t)(d.mp / CUT) * (uint32_t)(d.np / CUT);
     for (uint32_t i = threadIdx.x; i < cuts; i += 256) p.cut_of[g.cut + i] = id;
     for (uint32_t i = threadIdx.x; i < g.parts; i += 256) p.part_of[g.part + i] = id;
@@ -201,11 +234,14 @@ __device__ __forceinline__ void cut_in_two(float x, _Float16& hi, _Float16& lo)
     lo = (_Float16)(x - (float)hi);
 }
 
-// Where element k of a row lies: in two parts, 32 hi and their 32 lo in turn.
+// Where element k of a row of an operand lies, in binary16 elements: the slabs of 128 rows stand one behind the other, so
+// what a product fetches at a time is contiguous.  In two parts, a row of a slab is 16 hi and their 16 lo.  `width`: elements
+// of a row.
 template <bool SPLIT>
-__device__ __forceinline__ int64_t place(int64_t row, int64_t width, int64_t k)
+__device__ __forceinline__ int64_t place(int row, int width, int k)
 {
-    return SPLIT ? row * width * 2 + (k >> 5) * 64 + (k & 31) : row * width + k;
+    constexpr int EACH = SPLIT ? 16 : 32, LOG = SPLIT ? 4 : 5;
+    return ((int64_t)(row >> 7) * (width >> LOG) + (k >> LOG)) * (BLOCK * 32) + (row & (BLOCK - 1)) * 32 + (k & (EACH - 1));
 }
 
 // X and X^T as operands, from the matrix over its norm; zeros in the padding.
@@ -248,7 +284,7 @@ __global__ __launch_bounds__(256) void cut_kernel(Call p)
         }
         const int64_t at = second ? place<SPLIT>(j0 + row, d.mp, i0 + k) : place<SPLIT>(i0 + row, d.np, j0 + k);
         *(half8*)((second ? xt : x) + at) = h;
-        if (SPLIT) *(half8*)((second ? xt : x) + at + 32) = l;
+        if (SPLIT) *(half8*)((second ? xt : x) + at + LOW) = l;
         else if (second) *(half8*)(lo + at) = l;
     }
 }
@@ -257,197 +293,277 @@ __global__ __launch_bounds__(256) void cut_kernel(Call p)
 // products
 // ---------------------------------------------------------------------------------------------------------------------
 
+// A value that is the same in all lanes, in scalar registers.
+template <typename S>
+__device__ __forceinline__ S uniform(S x)
+{
+    static_assert(sizeof(S) % 4 == 0, "whole words");
+    uint32_t words[sizeof(S) / 4];
+    __builtin_memcpy(words, &x, sizeof(S));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(S) / 4); ++i) words[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)words[i]);
+    __builtin_memcpy(&x, words, sizeof(S));
+    return x;
+}
+
 enum Product { GRAM, POLY, NEXT, LAST };   // A; P; X of the next step; X of the last one, into the caller's buffers
 
-// C = L R^T on tiles of 128 x 128, four wavefronts of 64 x 64.  An operand's tile is 128 rows of SLAB bytes in LDS, fetched
-// there without passing through registers; the 16-byte chunks of a row are stored in an order turned by the row, so that
-// the lanes that read one chunk of eight consecutive rows touch all banks.
-template <Product PRODUCT, bool SPLIT, typename E, bool UPDATE>
-__global__ __launch_bounds__(256, 2) void product_kernel(Call p)
+// Sixteen rows of a slab from global memory into LDS without a register in between, 16 bytes per lane; AT is added to both
+// addresses.  The LDS address is the wavefront's.  The compiler does not count these loads (arrived() does), and nothing
+// else in the kernel uses M0.
+template <int AT>
+__device__ __forceinline__ void fetch_16(const char* base, uint32_t offset, uint32_t lds)
 {
-    __shared__ __attribute__((aligned(16))) char lds[2][2][T * SLAB];
-    const Tile t = p.tiles[PRODUCT == GRAM ? 0 : PRODUCT == POLY ? 1 : 2][blockIdx.x];
-    const Mat& d = p.mats[t.mat];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" :: "s"(lds), "v"(offset), "s"(base), "n"(AT) : "memory");
+}
+
+// Waits until at most N of the wavefront's loads are under way, then for the workgroup's other wavefronts.
+template <int N>
+__device__ __forceinline__ void arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(N) : "memory");
+}
+
+__device__ __forceinline__ void cut_8(const float (&v)[8], half8& h, half8& l)
+{
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        _Float16 hi, lo;
+        cut_in_two(v[q], hi, lo);
+        h[q] = hi; l[q] = lo;
+    }
+}
+
+// C = L R^T on tiles of 64 F x 64 F, four wavefronts of 32 F x 32 F.  A slab of an operand is 64 F rows of SLAB bytes in LDS;
+// the 16-byte chunks of a row are stored in an order turned by the row, so that the lanes that read one chunk of eight
+// consecutive rows touch all banks.  While a slab is multiplied from registers, the next is read from LDS into others and
+// those behind it are on their way from memory, BUFFERS - 2 of them.
+template <Product PRODUCT, bool SPLIT, typename E, bool UPDATE, int F, int BUFFERS>
+__global__ __launch_bounds__(256, 1) void product_kernel(Call p)
+{
+    constexpr int T = 64 * F, LOADS = 2 * F;              // a wavefront's loads per slab
+    constexpr int SIDE = 64, PITCH = SIDE + 1;            // the epilogue goes through LDS in blocks of 64 x 64
+    constexpr int SLABS_BYTES = BUFFERS * 2 * T * SLAB, EPILOGUE_BYTES = 4 * SIDE * PITCH * 4;
+    __shared__ __attribute__((aligned(1024))) char lds[SLABS_BYTES > EPILOGUE_BYTES ? SLABS_BYTES : EPILOGUE_BYTES];
+    const Tile t = uniform(p.tiles[PRODUCT == GRAM ? 0 : PRODUCT == POLY ? 1 : 2][blockIdx.x]);
+    const Mat d = uniform(p.mats[t.mat]);
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int mp = d.mp, width = PRODUCT == GRAM ? d.np : mp;   // length of the sums
     const int64_t left = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : d.xt[p.flip];
     const int64_t right = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : d.q;
-    const int64_t row_bytes = (int64_t)width * (SPLIT ? 4 : 2);
-    const int slabs = (int)(row_bytes / SLAB);
+    const int slabs = width / (SPLIT ? 16 : 32);
 
-    // a wavefront fetches 32 rows of each operand, eight with one instruction: lane l fetches for row l / 8 the chunk whose
-    // place is l % 8
-    const int fetch_row = lane >> 3, fetch_chunk = (lane & 7) ^ (fetch_row & 7);
-    const char* from[2];
-    from[0] = p.ws + left + (int64_t)(t.i * T + w * 32 + fetch_row) * row_bytes + fetch_chunk * 16;
-    from[1] = p.ws + right + (int64_t)(t.j * T + w * 32 + fetch_row) * row_bytes + fetch_chunk * 16;
-    auto fetch = [&](int slab, int buffer) {
-#pragma unroll
-        for (int o = 0; o < 2; ++o)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void*)(from[o] + (int64_t)slab * SLAB + q * 8 * row_bytes),
-                    (__attribute__((address_space(3))) void*)(&lds[buffer][o][(w * 32 + q * 8) * SLAB]), 16, 0, 0);
+    // a wavefront fetches 16 F rows of each operand, sixteen with one instruction: lane l fetches for row l / 4 the chunk
+    // whose place is l % 4
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    const uint32_t fetch_at = (uint32_t)((lane >> 2) * SLAB + ((lane & 3) ^ ((lane >> 4) & 3)) * 16);
+    const char* from_left = uniform(p.ws + left + 2 * place<SPLIT>(t.i * T + w * 16 * F, width, 0));
+    const char* from_right = uniform(p.ws + right + 2 * place<SPLIT>(t.j * T + w * 16 * F, width, 0));
+    const uint32_t fetch_to = lds0 + (uint32_t)(w * 16 * F) * SLAB;
+    // load number `q` of a slab's 2 F (behind the last slab: of that one again, so that as many are always under way)
+    auto fetch = [&](int slab, int q) {
+        const int64_t at = (int64_t)(slab < slabs ? slab : slabs - 1) * (BLOCK * SLAB);
+        const uint32_t to = fetch_to + (uint32_t)((slab & (BUFFERS - 1)) * 2 * T * SLAB);
+        constexpr int ROWS = 16 * SLAB;
+        if (q == 0) fetch_16<0>(from_left + at, fetch_at, to);
+        if (q == 1) fetch_16<ROWS>(from_left + at, fetch_at, to);
+        if (F == 4 && q == 2) fetch_16<2 * ROWS>(from_left + at, fetch_at, to);
+        if (F == 4 && q == 3) fetch_16<3 * ROWS>(from_left + at, fetch_at, to);
+        if (q == F) fetch_16<0>(from_right + at, fetch_at, to + T * SLAB);
+        if (q == F + 1) fetch_16<ROWS>(from_right + at, fetch_at, to + T * SLAB);
+        if (F == 4 && q == F + 2) fetch_16<2 * ROWS>(from_right + at, fetch_at, to + T * SLAB);
+        if (F == 4 && q == F + 3) fetch_16<3 * ROWS>(from_right + at, fetch_at, to + T * SLAB);
     };
-    const int wi = (w >> 1) * 64, wj = (w & 1) * 64;
+    const int wi = (w >> 1) * 32 * F, wj = (w & 1) * 32 * F;
     const int frag_row = lane & 31, frag_half = lane >> 5;
-    auto fragment = [&](int buffer, int o, int row0, int chunk) {
-        const int row = row0 + frag_row;
-        return *(const half8*)&lds[buffer][o][row * SLAB + ((chunk + frag_half) ^ (row & 7)) * 16];
+    // a slab's fragments: two each of 32 rows by 16 elements (SPLIT: hi and lo of the same)
+    half8 l[2][2][F], r[2][2][F];
+    const int chunk0 = (frag_half ^ ((frag_row >> 2) & 3)) * 16, chunk1 = chunk0 ^ 32;
+    // fragment number `q` of a slab's 4 F, in the order of their use
+    auto read = [&](int slab, int set, int q) {
+        const char* at = lds + (slab & (BUFFERS - 1)) * 2 * T * SLAB + frag_row * SLAB;
+        const int h = q / (2 * F), i = q % F, o = q / F % 2;
+        const int part = SPLIT && o ? 1 - h : h;      // the first product takes hi of the left and lo of the right
+        const char* from = at + (part ? chunk1 : chunk0) + (o ? T + wj + i * 32 : wi + i * 32) * SLAB;
+        if (o) r[set][part][i] = *(const half8*)from;
+        else l[set][part][i] = *(const half8*)from;
     };
-    float16v acc[2][2];
+    float16v acc[F][F];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < F; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < F; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
 
-    fetch(0, 0);
-    for (int s = 0; s < slabs; ++s) {
-        __syncthreads();   // this slab has arrived, and every wavefront is done with the one before
-        half8 l[2][4], r[2][4];
+    static_assert((BUFFERS & (BUFFERS - 1)) == 0 && BUFFERS >= 4, "slabs in turn");
+    for (int s = 0; s < BUFFERS - 1; ++s)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int q = 0; q < 2 * F; ++q) fetch(s, q);
+    arrived<(BUFFERS - 2) * LOADS>();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                l[i][k] = fragment(s & 1, 0, wi + i * 32, k * 2);
-                r[i][k] = fragment(s & 1, 1, wj + i * 32, k * 2);
+    for (int q = 0; q < 4 * F; ++q) read(0, 0, q);
+    // The matrix instructions of a slab, with what brings in the others between them: a wavefront is alone on its SIMD, so
+    // what stands between two blocks of matrix instructions would leave the matrix core idle (in one block each, it was
+    // busy 61 % of the time).
+    constexpr int PRODUCTS = SPLIT ? 3 : 2, INSTS = PRODUCTS * F * F, ITEMS = 6 * F;
+    // (sides are padded to 128 elements of two bytes or more: an even number of slabs)
+    for (int s0 = 0; s0 < slabs; s0 += 2)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int s = s0 + u;
+            // slab s + 1 has arrived, those behind it may be on their way, and every wavefront is done with slab s - 1
+            arrived<(BUFFERS - 3) * LOADS>();
+#pragma unroll
+            for (int m = 0; m < INSTS; ++m) {
+#pragma unroll
+                for (int q = m * ITEMS / INSTS; q < (m + 1) * ITEMS / INSTS; ++q) {
+                    if (q % 3 == 0) fetch(s + BUFFERS - 1, q / 3);
+                    else read(s + 1, 1 - u, q - q / 3 - 1);
+                }
+                const int k = m / (F * F), i = m / F % F, j = m % F;
+                const int a = SPLIT ? (k == 1 ? 1 : 0) : k, b = SPLIT ? (k == 0 ? 1 : 0) : k;
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[u][a][i], r[u][b][j], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
-        if (s + 1 < slabs) fetch(s + 1, (s + 1) & 1);
-        if (SPLIT) {
-            // chunks 0 - 3 are hi, 4 - 7 lo: two steps of 16
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][k], r[j][k + 2], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][k + 2], r[j][k], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][k], r[j][k], acc[i][j], 0, 0, 0);
-                    }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][k], r[j][k], acc[i][j], 0, 0, 0);
         }
-    }
+    arrived<0>();   // nothing more comes, and the LDS of the slabs is free
 
-    // acc[i][j][4 g + q] of lane l is row 8 g + 4 (l / 32) + q, column l % 32 of its 32 x 32
-    const float* da = (const float*)(p.ws + d.da);
-    const float* dq = (const float*)(p.ws + d.dq);
+    // A wavefront puts 64 x 64 of its sums at a time into LDS and reads them back by rows, eight columns per lane, for the
+    // rest of the arithmetic with 16-byte accesses; what it writes in the other orientation goes through LDS once more.
+    float* block = (float*)lds + w * SIDE * PITCH;
+    char* ws = p.ws;
 #pragma unroll
-    for (int ti = 0; ti < 2; ++ti)
+    for (int bi = 0; bi < F / 2; ++bi)
 #pragma unroll
-        for (int tj = 0; tj < 2; ++tj)
+        for (int bj = 0; bj < F / 2; ++bj) {
+            const int i0 = t.i * T + wi + bi * SIDE, j0 = t.j * T + wj + bj * SIDE;
+            // acc[4 g + q] of lane l is row 8 g + 4 (l / 32) + q, column l % 32 of its 32 x 32
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int row = t.i * T + wi + ti * 32 + g * 8 + frag_half * 4;   // and the three behind it
-                const int col = t.j * T + wj + tj * 32 + frag_row;
-                float v[4];
+            for (int ti = 0; ti < 2; ++ti)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = acc[ti][tj][g * 4 + q];
-                if (PRODUCT == GRAM || PRODUCT == POLY) {
-                    // symmetric: (row, col) is written at (col, row), and at (row, col) too if that is another tile
-                    _Float16* to = (_Float16*)(p.ws + (PRODUCT == GRAM ? d.e : d.q));
-                    const int64_t at = place<SPLIT>(col, mp, row);
-                    if (PRODUCT == GRAM) {
-                        const float f = d.sa / (d.sx * d.sx);
+                for (int tj = 0; tj < 2; ++tj)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            v[q] *= f;
-                            if (row + q == col) {
-                                ((float*)(p.ws + d.da))[col] = v[q] / d.sa;
-                                v[q] = 0.0f;
-                            }
-                        }
-                    } else {
-                        const _Float16* e = (const _Float16*)(p.ws + d.e);
-                        const half4 eh = *(const half4*)(e + at);
-                        half4 el = {0, 0, 0, 0};
-                        if (SPLIT) el = *(const half4*)(e + at + 32);
-                        const float dj = da[col], sa = 1.0f / d.sa;
+                    for (int r = 0; r < 16; ++r)
+                        block[(ti * 32 + (r >> 2) * 8 + frag_half * 4 + (r & 3)) * PITCH + tj * 32 + frag_row] = acc[bi * 2 + ti][bj * 2 + tj][r];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int part = (lane & 7) * 8;
+            bool other;   // whether the other orientation is wanted
+            if (PRODUCT == GRAM || PRODUCT == POLY) other = t.i != t.j;
+            else if (PRODUCT == NEXT) other = true;
+            else other = !d.tall;
+            for (int it = 0; it < SIDE / 8; ++it) {
+                const int i = i0 + it * 8 + (lane >> 3), j = j0 + part;
+                float* mine = block + (it * 8 + (lane >> 3)) * PITCH + part;
+                float v[8];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const float di = da[row + q], eij = ((float)eh[q] + (float)el[q]) * sa;
-                            float aa = v[q] * (sa * sa) + (di + dj) * eij;
-                            if (row + q == col) {
-                                aa += di * di;
-                                ((float*)(p.ws + d.dq))[col] = p.b * di + p.c * aa;
-                                v[q] = 0.0f;
-                            } else {
-                                v[q] = (p.b * eij + p.c * aa) * d.sq;
-                            }
+                for (int q = 0; q < 8; ++q) v[q] = mine[q];
+                const int64_t at = place<SPLIT>(i, mp, j);
+                half8 h, l;
+                if (PRODUCT == GRAM) {
+                    const float f = d.sa / (d.sx * d.sx);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        v[q] *= f;
+                        if (i == j + q) {
+                            ((float*)(ws + d.da))[i] = v[q] / d.sa;
+                            v[q] = 0.0f;
                         }
                     }
-                    half4 h, l;
+                    cut_8(v, h, l);
+                    _Float16* to = (_Float16*)(ws + d.e);
+                    *(half8*)(to + at) = h;
+                    if (SPLIT) *(half8*)(to + at + LOW) = l;
+                } else if (PRODUCT == POLY) {
+                    const _Float16* e = (const _Float16*)(ws + d.e);
+                    const half8 eh = *(const half8*)(e + at);
+                    half8 el = {0, 0, 0, 0, 0, 0, 0, 0};
+                    if (SPLIT) el = *(const half8*)(e + at + LOW);
+                    const float* da = (const float*)(ws + d.da);
+                    const float di = da[i], sa = 1.0f / d.sa;
+                    float dj[8];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        _Float16 hi, lo;
-                        cut_in_two(v[q], hi, lo);
-                        h[q] = hi; l[q] = lo;
-                    }
-                    *(half4*)(to + at) = h;
-                    if (SPLIT) *(half4*)(to + at + 32) = l;
-                    if (t.i != t.j) {
+                    for (int q = 0; q < 8; ++q) dj[q] = da[j + q];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int64_t other = place<SPLIT>(row + q, mp, col);
-                            to[other] = h[q];
-                            if (SPLIT) to[other + 32] = l[q];
+                    for (int q = 0; q < 8; ++q) {
+                        const float eij = ((float)eh[q] + (float)el[q]) * sa;
+                        float aa = v[q] * (sa * sa) + (di + dj[q]) * eij;
+                        v[q] = (p.b * eij + p.c * aa) * d.sq;
+                        if (i == j + q) {
+                            ((float*)(ws + d.dq))[i] = p.b * di + p.c * (aa + di * di);
+                            v[q] = 0.0f;
                         }
                     }
+                    cut_8(v, h, l);
+                    _Float16* to = (_Float16*)(ws + d.q);
+                    *(half8*)(to + at) = h;
+                    if (SPLIT) *(half8*)(to + at + LOW) = l;
                 } else {
-                    // row: along n, col: along m
-                    const _Float16* xt = (const _Float16*)(p.ws + d.xt[p.flip]);
-                    const float f = p.a + dq[col], sq = 1.0f / d.sq;
+                    // i: along n, j: along m
+                    const _Float16* xt = (const _Float16*)(ws + d.xt[p.flip]);
+                    const half8 xh = *(const half8*)(xt + at);
+                    const half8 xl = SPLIT ? *(const half8*)(xt + at + LOW) : *(const half8*)((const _Float16*)(ws + d.lo) + at);
+                    const float* dq = (const float*)(ws + d.dq);
+                    const float sq = 1.0f / d.sq;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int64_t at = place<SPLIT>(row + q, mp, col);
-                        const float lo = (float)(SPLIT ? xt[at + 32] : ((const _Float16*)(p.ws + d.lo))[at]);
-                        v[q] = f * ((float)xt[at] + lo) + v[q] * sq;
-                    }
+                    for (int q = 0; q < 8; ++q) v[q] = (p.a + dq[j + q]) * ((float)xh[q] + (float)xl[q]) + v[q] * sq;
                     if (PRODUCT == NEXT) {
-                        _Float16* x = (_Float16*)(p.ws + d.x);
-                        _Float16* next = (_Float16*)(p.ws + d.xt[1 - p.flip]);
-                        half4 h, l;
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            _Float16 hi, lo;
-                            cut_in_two(v[q], hi, lo);
-                            h[q] = hi; l[q] = lo;
-                            const int64_t at = place<SPLIT>(row + q, mp, col);
-                            next[at] = hi;
-                            if (SPLIT) next[at + 32] = lo;
-                            else ((_Float16*)(p.ws + d.lo))[at] = lo;
-                        }
-                        const int64_t at = place<SPLIT>(col, d.np, row);
-                        *(half4*)(x + at) = h;
-                        if (SPLIT) *(half4*)(x + at + 32) = l;
-                    } else if (col < d.m) {
+                        cut_8(v, h, l);
+                        _Float16* to = (_Float16*)(ws + d.xt[1 - p.flip]);
+                        *(half8*)(to + at) = h;
+                        if (SPLIT) *(half8*)(to + at + LOW) = l;
+                        else *(half8*)((_Float16*)(ws + d.lo) + at) = l;
+                    } else {
                         const float sx = 1.0f / d.sx, step = p.alpha * d.scale;
-                        typename E::word* out = (typename E::word*)p.out + d.offset;
-                        const int64_t along = d.tall ? d.stride : 1;
-                        int64_t at = d.tall ? (int64_t)row * d.stride + col : (int64_t)col * d.stride + row;
 #pragma unroll
-                        for (int q = 0; q < 4; ++q, at += along) {
-                            if (row + q >= d.n) break;
-                            float o = v[q] * sx;
+                        for (int q = 0; q < 8; ++q) v[q] = UPDATE ? step * (v[q] * sx) : v[q] * sx;
+                        if (!other && i < d.n && j < d.m) {
+                            typename E::word* out = (typename E::word*)p.out + d.offset + (int64_t)i * d.stride + j;
                             if (UPDATE) {
-                                o = step * o;
-                                o = p.keep * to_float<E>(out[at]) + o;
+                                float old[8];
+                                load_part<E, 8>(out, d.m - j, old);
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) v[q] = p.keep * old[q] + v[q];
                             }
-                            out[at] = from_float<E>(o);
+                            store_part<E, 8>(out, d.m - j, v);
                         }
                     }
                 }
+                if (other) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) mine[q] = v[q];
+                }
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (other)
+                for (int it = 0; it < SIDE / 8; ++it) {
+                    const int j = j0 + it * 8 + (lane >> 3), i = i0 + part;
+                    const float* mine = block + part * PITCH + it * 8 + (lane >> 3);
+                    float v[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] = mine[q * PITCH];
+                    if (PRODUCT == LAST) {
+                        if (i < d.n && j < d.m) {
+                            typename E::word* out = (typename E::word*)p.out + d.offset + (int64_t)j * d.stride + i;
+                            if (UPDATE) {
+                                float old[8];
+                                load_part<E, 8>(out, d.n - i, old);
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) v[q] = p.keep * old[q] + v[q];
+                            }
+                            store_part<E, 8>(out, d.n - i, v);
+                        }
+                    } else {
+                        half8 h, l;
+                        cut_8(v, h, l);
+                        const int64_t at = place<SPLIT>(j, PRODUCT == NEXT ? d.np : mp, i);
+                        _Float16* to = (_Float16*)(ws + (PRODUCT == GRAM ? d.e : PRODUCT == POLY ? d.q : d.x));
+                        *(half8*)(to + at) = h;
+                        if (SPLIT) *(half8*)(to + at + LOW) = l;
+                    }
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -458,6 +574,7 @@ constexpr int64_t MAX_SIDE = 1 << 20, MAX_SMALL_SIDE = 32768, MAX_FLAT = 1LL << 
 constexpr uint64_t MAX_TILES = 1u << 24;
 
 struct Layout {
+    int tile;            // side of a tile
     uint64_t tiles[3], cuts, parts;
     int64_t mats, tile_at[3], part_sums, cut_of, part_of, data, total;
 };
@@ -466,6 +583,26 @@ int parts_of(int64_t rows, int64_t cols)
 {
     const int64_t n = (rows * cols + PART - 1) / PART;
     return (int)(n < MAX_PARTS ? n : MAX_PARTS);
+}
+
+// Side of the products' tiles.  Tiles of 256 feed the matrix cores with half the LDS traffic of those of 128, but there are a
+// quarter as many and more of them is padding.
+int tile_of(const int64_t* matrices, int n_mat)
+{
+    double cost[2];
+    for (int k = 0; k < 2; ++k) {
+        const int tile = k ? 256 : 128;
+        double work = 0.0, longest = 0.0;   // of the product with X, in units of a tile of 128 and 128 elements of its sum
+        for (int i = 0; i < n_mat; ++i) {
+            const double m = (double)padded(std::min(matrices[4 * i + 1], matrices[4 * i + 2]), tile) / 128.0;
+            const double n = (double)padded(std::max(matrices[4 * i + 1], matrices[4 * i + 2]), tile) / 128.0;
+            const double one = (k ? 4.0 : 1.5);   // time of a tile of this size
+            work += n * m * m * (k ? 1.0 : 1.5) * 1.5;
+            longest = std::max(longest, n * one);
+        }
+        cost[k] = std::max(work / 256.0, longest);
+    }
+    return cost[1] < cost[0] ? 256 : 128;
 }
 
 // matrices: {offset, rows, cols, stride} each.
@@ -477,12 +614,15 @@ bool lay_out_all(const int64_t* matrices, int n_mat, bool split, Layout& L)
         const int64_t rows = matrices[4 * i + 1], cols = matrices[4 * i + 2], stride = matrices[4 * i + 3];
         if (rows < 1 || cols < 1 || rows > MAX_SIDE || cols > MAX_SIDE || stride < cols || stride > MAX_FLAT) return false;
         if (rows > MAX_SMALL_SIDE && cols > MAX_SMALL_SIDE) return false;
+    }
+    L.tile = tile_of(matrices, n_mat);
+    for (int i = 0; i < n_mat; ++i) {
         Mat d;
-        data += lay_out(d, rows, cols, 0, split);
-        const uint64_t tm = d.mp / T, tn = d.np / T;
+        data += lay_out(d, matrices[4 * i + 1], matrices[4 * i + 2], 0, split, L.tile);
+        const uint64_t tm = d.mp / L.tile, tn = d.np / L.tile;
         L.tiles[0] += tm * (tm + 1) / 2; L.tiles[1] += tm * (tm + 1) / 2; L.tiles[2] += tm * tn;
         L.cuts += (uint64_t)(d.mp / CUT) * (uint64_t)(d.np / CUT);
-        L.parts += parts_of(rows, cols);
+        L.parts += parts_of(matrices[4 * i + 1], matrices[4 * i + 2]);
         if (L.tiles[0] > MAX_TILES || L.tiles[2] > MAX_TILES || L.cuts > MAX_TILES) return false;
     }
     int64_t at = 0;
@@ -555,6 +695,23 @@ bool bounded(const double* coefficients, int steps)
 
 constexpr double QUINTIC[3] = {3.4445, -4.7750, 2.0315};
 
+template <typename E, bool UPDATE, bool SPLIT, int F, int BUFFERS>
+void launch_products(Call& p, const Layout& L, int steps, const double* coefficients, hipStream_t stream)
+{
+    const dim3 grid[3] = {(uint32_t)L.tiles[0], (uint32_t)L.tiles[1], (uint32_t)L.tiles[2]};
+    for (int k = 0; k < steps; ++k) {
+        const double* c = coefficients ? coefficients + 3 * k : QUINTIC;
+        p.a = (float)c[0]; p.b = (float)c[1]; p.c = (float)c[2];
+        p.flip = k & 1;
+        hipLaunchKernelGGL((product_kernel<GRAM, SPLIT, F32, false, F, BUFFERS>), grid[0], dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((product_kernel<POLY, SPLIT, F32, false, F, BUFFERS>), grid[1], dim3(256), 0, stream, p);
+        if (k + 1 < steps)
+            hipLaunchKernelGGL((product_kernel<NEXT, SPLIT, F32, false, F, BUFFERS>), grid[2], dim3(256), 0, stream, p);
+        else
+            hipLaunchKernelGGL((product_kernel<LAST, SPLIT, E, UPDATE, F, BUFFERS>), grid[2], dim3(256), 0, stream, p);
+    }
+}
+
 template <typename E, bool UPDATE, bool SPLIT>
 int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, int n_mat, int steps, const double* coefficients,
         hipStream_t stream)
@@ -568,9 +725,9 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
     std::sort(by_n, by_n + n_mat, [&](int a, int b) { return large(a) != large(b) ? large(a) > large(b) : a < b; });
     uint32_t tile[3][MAX_MAT], at[3] = {0, 0, 0};
     for (int q = 0; q < n_mat; ++q) {
-        const uint32_t n0 = (uint32_t)(padded(small(by_n[q])) / T);
+        const uint32_t n0 = (uint32_t)(padded(small(by_n[q]), L.tile) / L.tile);
         tile[0][by_n[q]] = at[0]; at[0] += n0 * (n0 + 1) / 2;
-        const uint32_t m0 = (uint32_t)(padded(small(by_m[q])) / T), m1 = (uint32_t)(padded(large(by_m[q])) / T);
+        const uint32_t m0 = (uint32_t)(padded(small(by_m[q]), L.tile) / L.tile), m1 = (uint32_t)(padded(large(by_m[q]), L.tile) / L.tile);
         tile[1][by_m[q]] = at[1]; at[1] += m0 * (m0 + 1) / 2;
         tile[2][by_m[q]] = at[2]; at[2] += m0 * m1;
     }
@@ -579,7 +736,7 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
     for (int first = 0; first < n_mat; first += PER_INIT) {
         InitArgs a;
         std::memset(&a, 0, sizeof(a));
-        a.first = first; a.n = std::min(PER_INIT, n_mat - first); a.split = SPLIT;
+        a.first = first; a.n = std::min(PER_INIT, n_mat - first); a.split = SPLIT; a.tile = L.tile;
         for (int k = 0; k < a.n; ++k) {
             const int i = first + k;
             MatIn& g = a.mat[k];
@@ -587,7 +744,7 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
             g.stride = matrices[4 * i + 3];
             for (int s = 0; s < 3; ++s) g.tile[s] = tile[s][i];
             Mat d;
-            g.base = base; base += lay_out(d, g.rows, g.cols, base, SPLIT);
+            g.base = base; base += lay_out(d, g.rows, g.cols, base, SPLIT, L.tile);
             g.cut = cut; cut += (uint32_t)(d.mp / CUT) * (uint32_t)(d.np / CUT);
             g.part = part; g.parts = (uint32_t)parts_of(g.rows, g.cols); part += g.parts;
             g.scale = scales ? scales[i] : 1.0f;
@@ -596,17 +753,8 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
     }
     hipLaunchKernelGGL((norm_kernel<E, UPDATE>), dim3((uint32_t)L.parts), dim3(256), 0, stream, p);
     hipLaunchKernelGGL((cut_kernel<E, UPDATE, SPLIT>), dim3((uint32_t)L.cuts), dim3(256), 0, stream, p);
-    for (int k = 0; k < steps; ++k) {
-        const double* c = coefficients ? coefficients + 3 * k : QUINTIC;
-        p.a = (float)c[0]; p.b = (float)c[1]; p.c = (float)c[2];
-        p.flip = k & 1;
-        hipLaunchKernelGGL((product_kernel<GRAM, SPLIT, F32, false>), dim3((uint32_t)L.tiles[0]), dim3(256), 0, stream, p);
-        hipLaunchKernelGGL((product_kernel<POLY, SPLIT, F32, false>), dim3((uint32_t)L.tiles[1]), dim3(256), 0, stream, p);
-        if (k + 1 < steps)
-            hipLaunchKernelGGL((product_kernel<NEXT, SPLIT, F32, false>), dim3((uint32_t)L.tiles[2]), dim3(256), 0, stream, p);
-        else
-            hipLaunchKernelGGL((product_kernel<LAST, SPLIT, E, UPDATE>), dim3((uint32_t)L.tiles[2]), dim3(256), 0, stream, p);
-    }
+    if (L.tile == 256) launch_products<E, UPDATE, SPLIT, 4, 4>(p, L, steps, coefficients, stream);
+    else launch_products<E, UPDATE, SPLIT, 2, 8>(p, L, steps, coefficients, stream);
     return hipGetLastError() == hipSuccess ? GRAVAC_OK : GRAVAC_ERR_HIP;
 }
 
