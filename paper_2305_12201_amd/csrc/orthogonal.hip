@@ -339,7 +339,7 @@ __device__ __forceinline__ void cut_8(const float (&v)[8], half8& h, half8& l)
 // consecutive rows touch all banks.  While a slab is multiplied from registers, the next is read from LDS into others and
 // those behind it are on their way from memory, BUFFERS - 2 of them.
 template <Product PRODUCT, bool SPLIT, typename E, bool UPDATE, int F, int BUFFERS>
-__global__ __launch_bounds__(256, 1) void product_kernel(Call p)
+__global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_kernel(Call p)
 {
     constexpr int T = 64 * F, LOADS = 2 * F;              // a wavefront's loads per slab
     constexpr int SIDE = 64, PITCH = SIDE + 1;            // the epilogue goes through LDS in blocks of 64 x 64
@@ -438,6 +438,36 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Call p)
 #pragma unroll
         for (int bj = 0; bj < F / 2; ++bj) {
             const int i0 = t.i * T + wi + bi * SIDE, j0 = t.j * T + wj + bj * SIDE;
+            const int part = (lane & 7) * 8, j = j0 + part;
+            // what the sums meet in memory, all of it under way before the first is used
+            constexpr int ROWS = SIDE / 8;
+            half8 mh[ROWS], ml[ROWS];
+            float mi[ROWS], mj[8];
+            if (PRODUCT == POLY) {
+                const _Float16* e = (const _Float16*)(ws + d.e);
+                const float* da = (const float*)(ws + d.da);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) mj[q] = da[j + q];
+#pragma unroll
+                for (int it = 0; it < ROWS; ++it) {
+                    const int i = i0 + it * 8 + (lane >> 3);
+                    const int64_t at = place<SPLIT>(i, mp, j);
+                    mi[it] = da[i];
+                    mh[it] = *(const half8*)(e + at);
+                    if (SPLIT) ml[it] = *(const half8*)(e + at + LOW);
+                }
+            } else if (PRODUCT == NEXT || PRODUCT == LAST) {
+                const _Float16* xt = (const _Float16*)(ws + (p.flip ? d.xt[1] : d.xt[0]));
+                const float* dq = (const float*)(ws + d.dq);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) mj[q] = p.a + dq[j + q];
+#pragma unroll
+                for (int it = 0; it < ROWS; ++it) {
+                    const int64_t at = place<SPLIT>(i0 + it * 8 + (lane >> 3), mp, j);
+                    mh[it] = *(const half8*)(xt + at);
+                    ml[it] = SPLIT ? *(const half8*)(xt + at + LOW) : *(const half8*)((const _Float16*)(ws + d.lo) + at);
+                }
+            }
             // acc[4 g + q] of lane l is row 8 g + 4 (l / 32) + q, column l % 32 of its 32 x 32
 #pragma unroll
             for (int ti = 0; ti < 2; ++ti)
@@ -447,13 +477,13 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Call p)
                     for (int r = 0; r < 16; ++r)
                         block[(ti * 32 + (r >> 2) * 8 + frag_half * 4 + (r & 3)) * PITCH + tj * 32 + frag_row] = acc[bi * 2 + ti][bj * 2 + tj][r];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const int part = (lane & 7) * 8;
             bool other;   // whether the other orientation is wanted
             if (PRODUCT == GRAM || PRODUCT == POLY) other = t.i != t.j;
             else if (PRODUCT == NEXT) other = true;
             else other = !d.tall;
-            for (int it = 0; it < SIDE / 8; ++it) {
-                const int i = i0 + it * 8 + (lane >> 3), j = j0 + part;
+#pragma unroll
+            for (int it = 0; it < ROWS; ++it) {
+                const int i = i0 + it * 8 + (lane >> 3);
                 float* mine = block + (it * 8 + (lane >> 3)) * PITCH + part;
                 float v[8];
 #pragma unroll
@@ -470,63 +500,43 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Call p)
                             v[q] = 0.0f;
                         }
                     }
-                    cut_8(v, h, l);
-                    _Float16* to = (_Float16*)(ws + d.e);
-                    *(half8*)(to + at) = h;
-                    if (SPLIT) *(half8*)(to + at + LOW) = l;
                 } else if (PRODUCT == POLY) {
-                    const _Float16* e = (const _Float16*)(ws + d.e);
-                    const half8 eh = *(const half8*)(e + at);
-                    half8 el = {0, 0, 0, 0, 0, 0, 0, 0};
-                    if (SPLIT) el = *(const half8*)(e + at + LOW);
-                    const float* da = (const float*)(ws + d.da);
-                    const float di = da[i], sa = 1.0f / d.sa;
-                    float dj[8];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) dj[q] = da[j + q];
+                    const float di = mi[it], sa = 1.0f / d.sa;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
-                        const float eij = ((float)eh[q] + (float)el[q]) * sa;
-                        float aa = v[q] * (sa * sa) + (di + dj[q]) * eij;
+                        const float eij = ((float)mh[it][q] + (SPLIT ? (float)ml[it][q] : 0.0f)) * sa;
+                        const float aa = v[q] * (sa * sa) + (di + mj[q]) * eij;
                         v[q] = (p.b * eij + p.c * aa) * d.sq;
                         if (i == j + q) {
                             ((float*)(ws + d.dq))[i] = p.b * di + p.c * (aa + di * di);
                             v[q] = 0.0f;
                         }
                     }
-                    cut_8(v, h, l);
-                    _Float16* to = (_Float16*)(ws + d.q);
-                    *(half8*)(to + at) = h;
-                    if (SPLIT) *(half8*)(to + at + LOW) = l;
                 } else {
                     // i: along n, j: along m
-                    const _Float16* xt = (const _Float16*)(ws + d.xt[p.flip]);
-                    const half8 xh = *(const half8*)(xt + at);
-                    const half8 xl = SPLIT ? *(const half8*)(xt + at + LOW) : *(const half8*)((const _Float16*)(ws + d.lo) + at);
-                    const float* dq = (const float*)(ws + d.dq);
                     const float sq = 1.0f / d.sq;
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = (p.a + dq[j + q]) * ((float)xh[q] + (float)xl[q]) + v[q] * sq;
-                    if (PRODUCT == NEXT) {
-                        cut_8(v, h, l);
-                        _Float16* to = (_Float16*)(ws + d.xt[1 - p.flip]);
-                        *(half8*)(to + at) = h;
-                        if (SPLIT) *(half8*)(to + at + LOW) = l;
-                        else *(half8*)((_Float16*)(ws + d.lo) + at) = l;
-                    } else {
-                        const float sx = 1.0f / d.sx, step = p.alpha * d.scale;
+                    for (int q = 0; q < 8; ++q) v[q] = mj[q] * ((float)mh[it][q] + (float)ml[it][q]) + v[q] * sq;
+                }
+                if (PRODUCT != LAST) {
+                    cut_8(v, h, l);
+                    _Float16* to = (_Float16*)(ws + (PRODUCT == GRAM ? d.e : PRODUCT == POLY ? d.q : p.flip ? d.xt[0] : d.xt[1]));
+                    *(half8*)(to + at) = h;
+                    if (SPLIT) *(half8*)(to + at + LOW) = l;
+                    else if (PRODUCT == NEXT) *(half8*)((_Float16*)(ws + d.lo) + at) = l;
+                } else {
+                    const float sx = 1.0f / d.sx, step = p.alpha * d.scale;
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) v[q] = UPDATE ? step * (v[q] * sx) : v[q] * sx;
-                        if (!other && i < d.n && j < d.m) {
-                            typename E::word* out = (typename E::word*)p.out + d.offset + (int64_t)i * d.stride + j;
-                            if (UPDATE) {
-                                float old[8];
-                                load_part<E, 8>(out, d.m - j, old);
+                    for (int q = 0; q < 8; ++q) v[q] = UPDATE ? step * (v[q] * sx) : v[q] * sx;
+                    if (!other && i < d.n && j < d.m) {
+                        typename E::word* out = (typename E::word*)p.out + d.offset + (int64_t)i * d.stride + j;
+                        if (UPDATE) {
+                            float old[8];
+                            load_part<E, 8>(out, d.m - j, old);
 #pragma unroll
-                                for (int q = 0; q < 8; ++q) v[q] = p.keep * old[q] + v[q];
-                            }
-                            store_part<E, 8>(out, d.m - j, v);
+                            for (int q = 0; q < 8; ++q) v[q] = p.keep * old[q] + v[q];
                         }
+                        store_part<E, 8>(out, d.m - j, v);
                     }
                 }
                 if (other) {
@@ -536,7 +546,8 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Call p)
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             if (other)
-                for (int it = 0; it < SIDE / 8; ++it) {
+#pragma unroll
+                for (int it = 0; it < ROWS; ++it) {
                     const int j = j0 + it * 8 + (lane >> 3), i = i0 + part;
                     const float* mine = block + part * PITCH + it * 8 + (lane >> 3);
                     float v[8];
@@ -695,20 +706,23 @@ bool bounded(const double* coefficients, int steps)
 
 constexpr double QUINTIC[3] = {3.4445, -4.7750, 2.0315};
 
-template <typename E, bool UPDATE, bool SPLIT, int F, int BUFFERS>
+template <typename E, bool UPDATE, bool SPLIT, int F>
 void launch_products(Call& p, const Layout& L, int steps, const double* coefficients, hipStream_t stream)
 {
+    // tiles of 128: two workgroups on a compute unit, one of which multiplies while the other starts or ends; the product with
+    // the longest sums has few tiles and takes one workgroup with twice the slabs under way (four 2600 x 650, ResNet101 shape:
+    // 140 -> 97 us of it)
     const dim3 grid[3] = {(uint32_t)L.tiles[0], (uint32_t)L.tiles[1], (uint32_t)L.tiles[2]};
     for (int k = 0; k < steps; ++k) {
         const double* c = coefficients ? coefficients + 3 * k : QUINTIC;
         p.a = (float)c[0]; p.b = (float)c[1]; p.c = (float)c[2];
         p.flip = k & 1;
-        hipLaunchKernelGGL((product_kernel<GRAM, SPLIT, F32, false, F, BUFFERS>), grid[0], dim3(256), 0, stream, p);
-        hipLaunchKernelGGL((product_kernel<POLY, SPLIT, F32, false, F, BUFFERS>), grid[1], dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((product_kernel<GRAM, SPLIT, F32, false, F, F == 4 ? 4 : 8>), grid[0], dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((product_kernel<POLY, SPLIT, F32, false, F, 4>), grid[1], dim3(256), 0, stream, p);
         if (k + 1 < steps)
-            hipLaunchKernelGGL((product_kernel<NEXT, SPLIT, F32, false, F, BUFFERS>), grid[2], dim3(256), 0, stream, p);
+            hipLaunchKernelGGL((product_kernel<NEXT, SPLIT, F32, false, F, 4>), grid[2], dim3(256), 0, stream, p);
         else
-            hipLaunchKernelGGL((product_kernel<LAST, SPLIT, E, UPDATE, F, BUFFERS>), grid[2], dim3(256), 0, stream, p);
+            hipLaunchKernelGGL((product_kernel<LAST, SPLIT, E, UPDATE, F, 4>), grid[2], dim3(256), 0, stream, p);
     }
 }
 
@@ -753,8 +767,8 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
     }
     hipLaunchKernelGGL((norm_kernel<E, UPDATE>), dim3((uint32_t)L.parts), dim3(256), 0, stream, p);
     hipLaunchKernelGGL((cut_kernel<E, UPDATE, SPLIT>), dim3((uint32_t)L.cuts), dim3(256), 0, stream, p);
-    if (L.tile == 256) launch_products<E, UPDATE, SPLIT, 4, 4>(p, L, steps, coefficients, stream);
-    else launch_products<E, UPDATE, SPLIT, 2, 8>(p, L, steps, coefficients, stream);
+    if (L.tile == 256) launch_products<E, UPDATE, SPLIT, 4>(p, L, steps, coefficients, stream);
+    else launch_products<E, UPDATE, SPLIT, 2>(p, L, steps, coefficients, stream);
     return hipGetLastError() == hipSuccess ? GRAVAC_OK : GRAVAC_ERR_HIP;
 }
 
