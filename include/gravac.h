@@ -355,7 +355,7 @@ int gravac_embedding_lookup(const void* table, int table_type, int64_t vocab, in
  *                   [0, vocab), such as -1, if there is no such token.
  *   table_grad      device, float[vocab][table_stride]; must not overlap grad_out.
  *   workspace       device, 256-byte aligned, at least gravac_embedding_gradient_workspace_bytes(n_tokens, vocab, dim)
- *                   bytes: 16 per token, and for calls of more than 128 tokens two rows of partial sums per 4 to 32 tokens.
+ *                   bytes: 16 per token, and two rows of partial sums per 4 to 32 tokens.
  *   flags           0 or GRAVAC_FLAG_ACCUMULATE.
  */
 int gravac_embedding_gradient_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, size_t* bytes_out);

@@ -54,6 +54,24 @@ __device__ __forceinline__ void store(typename E::word* p, const float (&x)[N])
     __builtin_memcpy((Pack<E, N>*)p, &v, sizeof(v));
 }
 
+// ... with the hint that the result is not read again soon
+template <typename E, int N>
+__device__ __forceinline__ void store_streaming(typename E::word* p, const float (&x)[N])
+{
+    constexpr int BYTES = N * E::SIZE, EACH = BYTES < 16 ? BYTES : 16;
+    typedef uint32_t words __attribute__((ext_vector_type(EACH / 4)));
+    typedef words places __attribute__((aligned(E::SIZE)));
+    typename E::word w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = from_float<E>(x[i]);
+#pragma unroll
+    for (int i = 0; i < BYTES / EACH; ++i) {
+        words v;
+        __builtin_memcpy(&v, (const char*)w + i * EACH, EACH);
+        __builtin_nontemporal_store(v, (places*)p + i);
+    }
+}
+
 // ... and the first `n` of them (the end of a row)
 template <typename E, int N>
 __device__ __forceinline__ void load_part(const typename E::word* p, int n, float (&x)[N])
@@ -71,6 +89,10 @@ __device__ __forceinline__ void store_part(typename E::word* p, int n, const flo
     for (int i = 0; i < N; ++i)
         if (i < n) p[i] = from_float<E>(x[i]);
 }
+
+// Results of more bytes than this are written with the hint that they are not read again soon: half of the 256 MB cache in
+// front of memory.  Smaller ones may still be there when the next call reads them.
+constexpr int64_t STREAM_BYTES = 128ll << 20;
 
 }  // namespace elements
 

@@ -37,6 +37,7 @@ struct LookupParams {
     int32_t dim;
     int32_t wide;    // tokens of 8 bytes
     int32_t lanes;   // lanes that share a row: a power of two up to 64
+    int32_t stream;  // see STREAM_BYTES
     float scale;
 };
 
@@ -69,7 +70,8 @@ __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p)
 #pragma unroll
                 for (int i = 0; i < N; ++i) x[k][i] *= p.scale;
             }
-            store_part<B, N>(to + c, p.dim - c, x[k]);
+            if (p.stream && p.dim - c >= N) store_streaming<B, N>(to + c, x[k]);   // (65,539 rows of 8 KiB: 215 -> 201 us)
+            else store_part<B, N>(to + c, p.dim - c, x[k]);
         }
     }
 }
@@ -110,8 +112,8 @@ constexpr int MAX_BITS = 9;                      // bits of a digit at most: two
 constexpr int MIN_BITS = 4;
 constexpr int BINS = 1 << MAX_BITS;
 constexpr int SORT_GRID = 128;                   // sorting workgroups at most: each adds up all workgroups' counts
-constexpr int FILL_GRID = 2048;                  // workgroups at most that clear the table beside the sort
-constexpr int FEW = 128;                         // calls of at most this many tokens are not sorted
+constexpr int FEW = 1024;                        // calls of at most this many tokens are not sorted
+constexpr int FEW_T = 256, FEW_W = FEW_T / 64;
 
 struct GradParams {
     const void* grad;
@@ -120,7 +122,6 @@ struct GradParams {
     int64_t n, grad_stride, table_stride;
     int64_t vocab, padding;
     int32_t dim, wide;
-    int32_t accumulate;
     float scale;
     uint2* pairs[2];       // (token or vocab, position): sorted, between two passes
     uint32_t* counts;      // [SORT_GRID][BINS]
@@ -131,6 +132,10 @@ struct GradParams {
     int64_t per_wg;        // tokens per sorting workgroup
     int32_t sort_wgs, bits, share_log;
     uint32_t n_shares;
+    int32_t fill_rows;     // rows of the table that a workgroup looks after, of those that no token names
+    uint32_t fill_wgs;     // such workgroups
+    uint32_t fills;        // ... along the grid
+    int32_t stream;        // see STREAM_BYTES
 };
 
 // The token at position i as a sort key: `vocab` for one that takes no part.
@@ -140,19 +145,35 @@ __device__ __forceinline__ uint32_t key_at(const GradParams& p, int64_t i)
     return t < 0 || t >= p.vocab || t == p.padding ? (uint32_t)p.vocab : (uint32_t)t;
 }
 
-// Clears the table: workgroup `wg` of `wgs`, T threads each.
-template <int T>
-__device__ void fill_table(const GradParams& p, int64_t wg, int64_t wgs)
+// A workgroup clears the rows that no token names of a block of fill_rows (at most 64, about FILL_ELEMENTS elements): all of
+// its threads write consecutive places, and workgroups that run together neighbouring blocks.  (A wavefront per row, the
+// rows of a workgroup far apart or not, wrote 2 to 4.7 TB/s, this 5.8.)  absent: a bit per row of the block.
+constexpr int64_t FILL_ELEMENTS = 16384;
+
+__device__ void clear_rows(const GradParams& p, int64_t row0, uint64_t absent)
 {
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (p.table_stride == p.dim) {
-        const int64_t n = p.vocab * p.dim;
-        for (int64_t i = (wg * T + threadIdx.x) * 4; i < n; i += wgs * T * 4)
-            store_part<F32, 4>((uint32_t*)p.table + i, n - i < 4 ? (int)(n - i) : 4, zero);
-    } else {
-        for (int64_t r = wg; r < p.vocab; r += wgs)
-            for (int c = (int)threadIdx.x * 4; c < p.dim; c += T * 4)
-                store_part<F32, 4>((uint32_t*)p.table + r * p.table_stride + c, p.dim - c, zero);
+    const int threads = (int)blockDim.x;
+    if (p.table_stride != p.dim || p.fill_rows == 1 || p.dim < 4) {
+        for (; absent; absent &= absent - 1) {
+            uint32_t* to = (uint32_t*)p.table + (row0 + __ffsll((unsigned long long)absent) - 1) * p.table_stride;
+            for (int c = (int)threadIdx.x * 4; c < p.dim; c += threads * 4) store_part<F32, 4>(to + c, p.dim - c, zero);
+        }
+        return;
+    }
+    uint32_t* to = (uint32_t*)p.table + row0 * p.dim;
+    const uint32_t n = (uint32_t)(p.vocab - row0 < p.fill_rows ? p.vocab - row0 : p.fill_rows) * (uint32_t)p.dim;
+    // x / dim as the upper half of a product: exact as long as x dim < 2^32, and x <= 4 FILL_ELEMENTS, dim <= 2 FILL_ELEMENTS
+    const uint32_t inverse = (uint32_t)(((1ull << 32) + p.dim - 1) / (uint32_t)p.dim);
+    auto clear = [&](uint32_t e) { return (absent >> __umulhi(e, inverse)) & 1; };
+    for (uint32_t e = threadIdx.x * 4; e < n; e += threads * 4) {
+        if (e + 3 < n && clear(e) && clear(e + 3)) {   // (two rows at most)
+            if (p.stream) store_streaming<F32, 4>(to + e, zero);
+            else store<F32, 4>(to + e, zero);
+        } else {
+            for (uint32_t i = e; i < e + 4 && i < n; ++i)
+                if (clear(i)) to[i] = 0;
+        }
     }
 }
 
@@ -223,15 +244,11 @@ __device__ void place_tile(SortLds& s, int bits, const uint32_t (&digit)[SORT_RO
     __syncthreads();
 }
 
-// A call of at most SORT_TILE tokens: workgroup 0 sorts them in LDS, the others clear the table meanwhile.
+// A call of at most SORT_TILE tokens: one workgroup sorts them in LDS.
 __global__ __launch_bounds__(SORT_T) void sort_few_kernel(GradParams p, int passes)
 {
     __shared__ SortLds s;
     __shared__ uint2 buf[SORT_TILE];
-    if (blockIdx.x != 0) {
-        fill_table<SORT_T>(p, (int64_t)blockIdx.x - 1, (int64_t)gridDim.x - 1);
-        return;
-    }
     if (threadIdx.x == 0) p.joins[0] = 0;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, bins = 1 << p.bits;
     uint2 x[SORT_ROUNDS];
@@ -276,36 +293,36 @@ __global__ __launch_bounds__(SORT_T) void sort_few_kernel(GradParams p, int pass
     }
 }
 
-// Larger calls, one pass: how often each digit occurs among a workgroup's tokens.  Before the first pass (from < 0) the
-// tokens come from the caller, and the workgroups behind the sorting ones clear the table.
+__device__ __forceinline__ uint32_t key_of(const GradParams& p, int from, int64_t i)   // from < 0: the caller's tokens
+{
+    return from < 0 ? key_at(p, i) : p.pairs[from][i].x;
+}
+
+// Larger calls, one pass: how often each digit occurs among a workgroup's tokens.
 __global__ __launch_bounds__(SORT_T) void count_kernel(GradParams p, int from, int shift)
 {
     __shared__ uint32_t cnt[BINS];
-    if ((int)blockIdx.x >= p.sort_wgs) {
-        fill_table<SORT_T>(p, (int64_t)blockIdx.x - p.sort_wgs, (int64_t)gridDim.x - p.sort_wgs);
-        return;
-    }
-    if (from < 0 && blockIdx.x == 0 && threadIdx.x == 0) p.joins[0] = 0;
     const int bins = 1 << p.bits;
     for (int i = threadIdx.x; i < bins; i += SORT_T) cnt[i] = 0;
     __syncthreads();
     const int64_t begin = blockIdx.x * p.per_wg, end = begin + p.per_wg < p.n ? begin + p.per_wg : p.n;
-    for (int64_t i = begin + threadIdx.x; i < end; i += SORT_T) {
-        const uint32_t key = from < 0 ? key_at(p, i) : p.pairs[from][i].x;
-        atomicAdd(&cnt[(key >> shift) & (bins - 1)], 1u);
-    }
+    for (int64_t i = begin + threadIdx.x; i < end; i += SORT_T) atomicAdd(&cnt[(key_of(p, from, i) >> shift) & (bins - 1)], 1u);
     __syncthreads();
     for (int i = threadIdx.x; i < bins; i += SORT_T) p.counts[(int64_t)blockIdx.x * BINS + i] = cnt[i];
 }
 
 // ... and the tokens moved to their places: behind all smaller digits, and behind the same digit of earlier workgroups.
+// (Workgroups that count all tokens themselves spare a launch per pass and take as long: 16,381 tokens 15.3 us instead of
+// 8.1 and 3 to 5 for the counts.)
 __global__ __launch_bounds__(SORT_T) void scatter_kernel(GradParams p, int from, int to, int shift)
 {
     __shared__ SortLds s;
     __shared__ uint32_t part[2][SORT_T];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, bins = 1 << p.bits;
     const int team = (int)threadIdx.x >> p.bits, teams = SORT_T >> p.bits, bin = threadIdx.x & (bins - 1);
+    const int64_t begin = blockIdx.x * p.per_wg, end = begin + p.per_wg < p.n ? begin + p.per_wg : p.n;
     uint32_t before = 0, all = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.joins[0] = 0;
 #pragma unroll 8
     for (int g = team; g < p.sort_wgs; g += teams) {
         const uint32_t c = p.counts[(int64_t)g * BINS + bin];
@@ -324,7 +341,6 @@ __global__ __launch_bounds__(SORT_T) void scatter_kernel(GradParams p, int from,
     const uint32_t first = exclusive_sum(all, s.wave);
     if ((int)threadIdx.x < bins) s.base[threadIdx.x] = first + before;
     __syncthreads();
-    const int64_t begin = blockIdx.x * p.per_wg, end = begin + p.per_wg < p.n ? begin + p.per_wg : p.n;
     for (int64_t t0 = begin; t0 < end; t0 += SORT_TILE) {
         uint2 x[SORT_ROUNDS];
         bool have[SORT_ROUNDS];
@@ -348,91 +364,157 @@ __global__ __launch_bounds__(SORT_T) void scatter_kernel(GradParams p, int from,
 // gradient: sums
 // ---------------------------------------------------------------------------------------------------------------------
 
-// A row's sum, scaled, into the table: written, or added to what is there.
-template <int N>
-__device__ __forceinline__ void put_row(const GradParams& p, uint32_t row, int c, const float (&sum)[N])
+// A row's sum, scaled, into the table: written, or added to what is there (`old`).
+template <bool ADD, int N>
+__device__ __forceinline__ void put_row(const GradParams& p, uint32_t row, int c, const float (&sum)[N], const float (&old)[N])
 {
-    uint32_t* to = (uint32_t*)p.table + (int64_t)row * p.table_stride + c;
     float x[N];
-    if (p.accumulate) {
-        load_part<F32, N>(to, p.dim - c, x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = x[i] + p.scale * sum[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = p.scale * sum[i];
-    }
-    store_part<F32, N>(to, p.dim - c, x);
+    for (int i = 0; i < N; ++i) x[i] = ADD ? old[i] + p.scale * sum[i] : p.scale * sum[i];
+    uint32_t* to = (uint32_t*)p.table + (int64_t)row * p.table_stride + c;
+    if (!ADD && p.stream && p.dim - c >= N) store_streaming<F32, N>(to, x);
+    else store_part<F32, N>(to, p.dim - c, x);
 }
 
-// A share of the sorted tokens (1 << share_log of them, at most 64: a lane holds one each) and 64 * N columns per wavefront.
-// Runs of one token that lie inside the share are written to the table; the sum of one that reaches over the share's begin or
-// end goes to the workspace, for join_kernel.
-template <typename E>
-__global__ __launch_bounds__(64) void sum_kernel(GradParams p, int sorted)
+template <bool ADD, int N>
+__device__ __forceinline__ void get_row(const GradParams& p, uint32_t row, int c, float (&old)[N])
+{
+    if (ADD) load_part<F32, N>((const uint32_t*)p.table + (int64_t)row * p.table_stride + c, p.dim - c, old);
+}
+
+// A share of the sorted tokens (1 << share_log of them, at most 64: a lane holds one each) per workgroup, 64 * N columns per
+// wavefront: a workgroup reads and writes whole rows, up to SUM_W wavefronts of them at a time.
+// The sum of a run of one token is written to the table by the wavefront of the share where it begins, which follows it into
+// the next share; only a run that covers a whole share is left in parts in the workspace, for join_kernel.  (All runs that
+// cross a share's end left to it: 131,072 tokens of a text give 2500 of them, and 146 us instead of 24.)
+// The first wavefronts clear the rows that no token names: a lane looks for one row among the sorted tokens, so that no row is
+// written twice (131,072 tokens on as many rows of 4096: 758 us, 1079 with all rows cleared beside the sort).
+constexpr int SUM_W = 8;
+
+// The place of the first sorted token that is not below `row`, by a wavefront that looks at 64 of them at a time.
+__device__ __forceinline__ uint32_t first_at_least(const uint2* pairs, uint32_t n, uint32_t row)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t lo = 0, hi = n;   // it lies in [lo, hi]
+    while (lo < hi) {
+        const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const uint32_t below = (uint32_t)__popcll(__ballot(at < hi && pairs[at].x < row));   // lanes 0 .. below - 1
+        if (below == 0) break;
+        hi = lo + below * step < hi ? lo + below * step : hi;
+        lo += (below - 1) * step + 1;
+    }
+    return lo;
+}
+
+template <typename E, bool ADD>
+__global__ __launch_bounds__(64 * SUM_W) void sum_kernel(GradParams p, int sorted)
 {
     constexpr int N = 16 / E::SIZE, U = 4;
-    const int lane = threadIdx.x;
-    const uint32_t share = blockIdx.x;
-    const int64_t i0 = (int64_t)share << p.share_log;
-    const uint32_t size = 1u << p.share_log, none = (uint32_t)p.vocab;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = (int)blockDim.x >> 6;
     const uint2* pairs = p.pairs[sorted];
-    uint2 mine = make_uint2(none, 0);
-    if (lane < (int)size && i0 + lane < p.n) mine = pairs[i0 + lane];
-    const uint32_t previous = i0 > 0 ? pairs[i0 - 1].x : none;
-    const uint32_t next = i0 + size < p.n ? pairs[i0 + size].x : none;
+    if (blockIdx.x < p.fills) {
+        const int64_t id = (int64_t)blockIdx.x * gridDim.y + blockIdx.y, r = id * p.fill_rows + lane;
+        const uint32_t row = (uint32_t)r;
+        bool named = lane >= p.fill_rows || id >= p.fill_wgs || r >= p.vocab;
+        if (id < p.fill_wgs) {
+            uint32_t lo = first_at_least(pairs, (uint32_t)p.n, (uint32_t)(id * p.fill_rows));
+            uint32_t hi = first_at_least(pairs, (uint32_t)p.n, (uint32_t)(id * p.fill_rows) + p.fill_rows);
+            if (!named) {
+                const uint32_t behind = hi;
+                while (lo < hi) {
+                    const uint32_t mid = lo + (hi - lo) / 2;
+                    if (pairs[mid].x < row) lo = mid + 1;
+                    else hi = mid;
+                }
+                named = lo < behind && pairs[lo].x == row;
+            }
+        }
+        clear_rows(p, id * p.fill_rows, ~__ballot(named));
+        return;
+    }
+    const uint32_t share = blockIdx.x - p.fills;
+    const int64_t i0 = (int64_t)share << p.share_log;
+    const int size = 1 << p.share_log;
+    const uint32_t none = (uint32_t)p.vocab;
+    uint2 mine = make_uint2(none, 0), behind = make_uint2(none, 0);
+    if (lane < size && i0 + lane < p.n) mine = pairs[i0 + lane];
+    if (lane < size && i0 + size + lane < p.n) behind = pairs[i0 + size + lane];
+    const uint32_t previous = i0 > 0 ? pairs[i0 - 1].x : none, before = i0 > 0 ? pairs[i0 - size].x : none;
     const int have = __popcll(__ballot(mine.x != none));
     if (have == 0) return;
-    const int c = ((int)blockIdx.y * 64 + lane) * N;
+    uint32_t row = __builtin_amdgcn_readlane(mine.x, 0);
+    const uint32_t last = __builtin_amdgcn_readlane(mine.x, have - 1);
+    const int head = __popcll(__ballot(mine.x == row));        // tokens of the first run that lie in this share
+    const int follow = have == size ? __popcll(__ballot(behind.x == last)) : 0;   // tokens of the last run in the next
+    int begin = 0, end = have;
+    bool to_head = false, to_tail = false;                      // the first run's or the last run's sum is a part
+    if (row == previous) {
+        if (head == size || before == row) to_head = true;      // the run covers this share or the one before
+        else begin = head;                                      // ... it is the share's before
+    }
+    if (!(to_head && head == size) && follow > 0) {
+        // (a run that fills this share and begins with it is in parts too)
+        if (follow == size || (row == last && head == size)) to_tail = true;
+        else end = have + follow;
+    }
+    if (begin == end) return;
+    const int c = (((int)blockIdx.y * waves + w) * 64 + lane) * N;
+    if (c - lane * N >= p.dim) return;
     const bool active = c < p.dim;
     const typename E::word* grad = (const typename E::word*)p.grad + c;
-    uint32_t row = __builtin_amdgcn_readlane(mine.x, 0);
-    bool first = true;
-    float sum[N];
+    if (to_tail && blockIdx.y == 0 && threadIdx.x == 0) p.joins[1 + atomicAdd(&p.joins[0], 1u)] = share;
+    row = __builtin_amdgcn_readlane(mine.x, begin < have ? begin : 0);
+    float sum[N], kept[N];   // kept: what the table holds in the row of the last token so far
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] = 0.0f;
 
-    auto flush = [&](bool last) {
-        if (first && previous == row) {
+    auto flush = [&](bool ends) {
+        if (to_head) {
             if (active) store_part<F32, N>((uint32_t*)p.head + (int64_t)share * p.part_stride + c, p.dim - c, sum);
-        } else if (last && next == row) {
+            to_head = false;
+        } else if (ends && to_tail) {
             if (active) store_part<F32, N>((uint32_t*)p.tail + (int64_t)share * p.part_stride + c, p.dim - c, sum);
-            if (blockIdx.y == 0 && lane == 0) p.joins[1 + atomicAdd(&p.joins[0], 1u)] = share;
         } else if (active) {
-            put_row<N>(p, row, c, sum);
+            put_row<ADD, N>(p, row, c, sum, kept);
         }
     };
-    for (int j0 = 0; j0 < have; j0 += U) {
-        float x[U][N];
+    auto token_of = [&](int j) { return (uint32_t)(j < have ? __builtin_amdgcn_readlane(mine.x, j) : __builtin_amdgcn_readlane(behind.x, (j - have) & 63)); };
+    auto place_of = [&](int j) { return (uint32_t)(j < have ? __builtin_amdgcn_readlane(mine.y, j) : __builtin_amdgcn_readlane(behind.y, (j - have) & 63)); };
+    for (int j0 = begin; j0 < end; j0 += U) {
+        float x[U][N], old[U][N];   // old: of the rows whose last token this is, all loads of a round together
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = j0 + u < have ? j0 + u : have - 1;
-            const uint32_t pos = __builtin_amdgcn_readlane(mine.y, j);
-            if (active) load_part<E, N>(grad + (int64_t)pos * p.grad_stride, p.dim - c, x[u]);
+            const int j = j0 + u < end ? j0 + u : end - 1;
+            if (active) load_part<E, N>(grad + (int64_t)place_of(j) * p.grad_stride, p.dim - c, x[u]);
+            if (ADD && active && (j + 1 == end || token_of(j + 1) != token_of(j))) get_row<ADD, N>(p, token_of(j), c, old[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (j0 + u >= have) break;
-            const uint32_t r = __builtin_amdgcn_readlane(mine.x, j0 + u);
+            if (j0 + u >= end) break;
+            const uint32_t r = token_of(j0 + u);
             if (r != row) {
                 flush(false);
                 row = r;
-                first = false;
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum[i] = 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) sum[i] += x[u][i];
+            if (ADD) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) kept[i] = old[u][i];
+            }
         }
     }
     flush(true);
 }
 
-// The runs that reach over shares: the tail of the share where one begins and the heads of the shares behind it, added up by
+// The runs that cover a share and more: the tail of the share where one begins and the heads of the shares behind it, added up by
 // eight wavefronts, each every eighth share in order, and these sums in order.
 constexpr int JOIN_W = 8;
 constexpr int JOIN_GRID = 1024;
 
+template <bool ADD>
 __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sorted)
 {
     constexpr int N = 4, U = 4;
@@ -481,7 +563,9 @@ __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sor
             for (int g = 0; g < JOIN_W; ++g)
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum[i] += lds[g][lane][i];
-            put_row<N>(p, row, c, sum);
+            float old[N];
+            get_row<ADD, N>(p, row, c, old);
+            put_row<ADD, N>(p, row, c, sum, old);
         }
         __syncthreads();
     }
@@ -491,56 +575,88 @@ __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sor
 // gradient: few tokens
 // ---------------------------------------------------------------------------------------------------------------------
 
-// At most FEW tokens, one launch: a wavefront per token (and 64 * N columns) looks at all of them; the first of its kind
-// adds up the rows of all of its kind, in order.  The wavefronts behind those clear the rows that no token names.
-template <typename E>
-__global__ __launch_bounds__(64) void sum_few_kernel(GradParams p)
+// At most FEW tokens, one launch: a workgroup per token (and 64 * N columns) looks at all of them; the first of its kind adds
+// up the rows of all of its kind, its wavefronts in turn, and their sums in order.  The first workgroups clear the rows
+// that no token names.  (700 tokens of 33,278 rows of 650: 16 us, 32 with a sort beside the
+// clearing and two more launches.)
+template <typename E, bool ADD>
+__global__ __launch_bounds__(FEW_T) void sum_few_kernel(GradParams p)
 {
     constexpr int N = 16 / E::SIZE, U = 4;
-    static_assert(FEW == 128, "two tokens per lane");
-    const int lane = threadIdx.x;
+    __shared__ uint32_t keys[FEW];
+    __shared__ float lds[FEW_W][64][N + 1];
+    __shared__ uint32_t named[64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const uint32_t none = (uint32_t)p.vocab;
-    const uint32_t k0 = lane < p.n ? key_at(p, lane) : none, k1 = lane + 64 < p.n ? key_at(p, lane + 64) : none;
-    if (blockIdx.x >= p.n) {
-        const int64_t wgs = (int64_t)gridDim.x - p.n;
-        const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int64_t r = ((int64_t)blockIdx.x - p.n) * gridDim.y + blockIdx.y; r < p.vocab; r += wgs * gridDim.y) {
-            if (__ballot(k0 == (uint32_t)r || k1 == (uint32_t)r)) continue;
-            for (int c = lane * 4; c < p.dim; c += 256)
-                store_part<F32, 4>((uint32_t*)p.table + r * p.table_stride + c, p.dim - c, zero);
+    if (blockIdx.x < p.fills) {
+        const uint32_t id = blockIdx.x * gridDim.y + blockIdx.y;
+        if (id >= p.fill_wgs) return;
+        if (threadIdx.x < 64) named[threadIdx.x] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.n; i += FEW_T) {
+            const uint32_t k = key_at(p, i);
+            if (k != none && k / p.fill_rows == id) named[k % p.fill_rows] = 1;
         }
+        __syncthreads();
+        const int64_t row0 = (int64_t)id * p.fill_rows;
+        clear_rows(p, row0, __ballot(lane < p.fill_rows && row0 + lane < p.vocab && !named[lane]));
         return;
     }
-    const int t = (int)blockIdx.x;
-    const uint32_t row = __builtin_amdgcn_readlane(t < 64 ? k0 : k1, t & 63);
-    uint64_t m0 = __ballot(k0 == row), m1 = __ballot(k1 == row);
-    const int leader = m0 ? __ffsll((unsigned long long)m0) - 1 : 64 + __ffsll((unsigned long long)m1) - 1;
-    if (row == none || leader != t) return;
+    const int groups = (int)((p.n + 63) / 64), t = (int)(blockIdx.x - p.fills);
+    for (int i = threadIdx.x; i < groups * 64; i += FEW_T) keys[i] = i < p.n ? key_at(p, i) : none;
+    __syncthreads();
+    const uint32_t row = keys[t];
+    if (row == none) return;
+    uint64_t seen = 0;   // of its kind, before it
+    for (int g = 0; g <= t / 64; ++g) {
+        const uint64_t before = t >= g * 64 + 64 ? ~0ull : (1ull << (t - g * 64)) - 1;
+        seen |= __ballot(keys[g * 64 + lane] == row) & before;
+    }
+    if (seen) return;
     const int c = ((int)blockIdx.y * 64 + lane) * N;
-    if (c >= p.dim) return;
+    const bool active = c < p.dim;
     const typename E::word* grad = (const typename E::word*)p.grad + c;
-    float sum[N];
+    float sum[N], old[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] = 0.0f;
-    while (m0 | m1) {
+    if (w == 0 && active) get_row<ADD, N>(p, row, c, old);
+    int at = 0, count = 0;   // how many of its kind have been seen, and how many of them wait to be added
+    int wait[U];
+    auto add = [&]() {
         float x[U][N];
-        bool have[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            have[u] = (m0 | m1) != 0;
-            int j = 0;
-            if (m0) { j = __ffsll((unsigned long long)m0) - 1; m0 &= m0 - 1; }
-            else if (m1) { j = 64 + __ffsll((unsigned long long)m1) - 1; m1 &= m1 - 1; }
-            if (have[u]) load_part<E, N>(grad + (int64_t)j * p.grad_stride, p.dim - c, x[u]);
-        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (have[u]) {
+            if (u < count && active) load_part<E, N>(grad + (int64_t)wait[u] * p.grad_stride, p.dim - c, x[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u < count) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum[i] += x[u][i];
             }
+        count = 0;
+    };
+    for (int g = t / 64; g < groups; ++g) {
+        uint64_t m = __ballot(keys[g * 64 + lane] == row);
+        for (; m; m &= m - 1, ++at) {
+            if (at % FEW_W != w) continue;
+            const int j = g * 64 + __ffsll((unsigned long long)m) - 1;
+#pragma unroll
+            for (int u = 0; u < U; ++u) wait[u] = u == count ? j : wait[u];
+            if (++count == U) add();
+        }
     }
-    put_row<N>(p, row, c, sum);
+    add();
+    if (at > 1) {   // the same for all wavefronts
+#pragma unroll
+        for (int i = 0; i < N; ++i) lds[w][lane][i] = sum[i];
+        __syncthreads();
+        if (w == 0)
+#pragma unroll
+            for (int v = 1; v < FEW_W; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] += lds[v][lane][i];
+    }
+    if (w == 0 && active) put_row<ADD, N>(p, row, c, sum, old);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -551,11 +667,11 @@ constexpr int64_t MAX_N = 2147483647LL, MAX_TOKENS = GRAVAC_EMBEDDING_MAX_TOKENS
 
 int share_log_of(int64_t n, int64_t dim)
 {
-    // tokens per share: the fewer, the more wavefronts; up to 32 once that leaves 8192 of them
+    // tokens per share: the fewer, the more wavefronts; the more, the fewer runs to join; up to 32 that leave 4096 of them
     const int64_t slabs = (dim + 511) / 512;
     int log = 2;
-    while (log < 5 && (n >> (log + 1)) * slabs >= 8192) ++log;
-    return log;
+    while (log < 5 && (n >> (log + 1)) * slabs >= 4096) ++log;
+    return (n >> log) > (1 << 24) ? 6 : log;   // (a lane holds a token; the grid has 32 bits)
 }
 
 struct GradLayout {
@@ -587,18 +703,21 @@ GradLayout grad_layout(int64_t n, int64_t dim)
     return L;
 }
 
-template <typename E>
+template <typename E, bool ADD>
 void launch_gradient(GradParams& p, const GradLayout& L, hipStream_t stream)
 {
     const uint32_t slabs = (uint32_t)((p.dim + 64 * (16 / E::SIZE) - 1) / (64 * (16 / E::SIZE)));
+    const uint32_t waves = p.n <= FEW ? FEW_W : slabs < SUM_W ? slabs : SUM_W;
+    const uint32_t columns = p.n <= FEW ? slabs : (slabs + waves - 1) / waves;   // workgroups side by side
+    if (!ADD) {
+        const int64_t rows = (p.n <= FEW ? 1 : 4) * FILL_ELEMENTS / p.dim;   // (four times as many to a search)
+        p.fill_rows = (int32_t)(rows < 1 ? 1 : rows > 64 ? 64 : rows);
+        p.fill_wgs = (uint32_t)((p.vocab + p.fill_rows - 1) / p.fill_rows);
+        p.fills = (p.fill_wgs + columns - 1) / columns;
+    }
     if (p.n <= FEW) {
-        int64_t fill = 0;
-        if (!p.accumulate) {
-            fill = (p.vocab + slabs - 1) / slabs;
-            if (fill > FILL_GRID) fill = FILL_GRID;
-        }
-        if (p.n + fill > 0)
-            hipLaunchKernelGGL(sum_few_kernel<E>, dim3((uint32_t)(p.n + fill), slabs), dim3(64), 0, stream, p);
+        if (p.n + p.fills > 0)
+            hipLaunchKernelGGL((sum_few_kernel<E, ADD>), dim3((uint32_t)p.n + p.fills, slabs), dim3(FEW_T), 0, stream, p);
         return;
     }
     int bits = 1;
@@ -606,30 +725,32 @@ void launch_gradient(GradParams& p, const GradLayout& L, hipStream_t stream)
     const int passes = (bits + MAX_BITS - 1) / MAX_BITS;
     p.bits = (bits + passes - 1) / passes;
     if (p.bits < MIN_BITS) p.bits = MIN_BITS;
-    int64_t fill = 0;
-    if (!p.accumulate) {
-        fill = (p.vocab * p.dim + 4 * SORT_T - 1) / (4 * SORT_T);
-        if (fill > FILL_GRID) fill = FILL_GRID;
-    }
     int sorted = 0;
     if (p.n <= SORT_TILE) {
-        hipLaunchKernelGGL(sort_few_kernel, dim3(1 + (uint32_t)fill), dim3(SORT_T), 0, stream, p, passes);
+        hipLaunchKernelGGL(sort_few_kernel, dim3(1), dim3(SORT_T), 0, stream, p, passes);
     } else {
         const int64_t tiles = (p.n + SORT_TILE - 1) / SORT_TILE;
         p.per_wg = (tiles + SORT_GRID - 1) / SORT_GRID * SORT_TILE;
         p.sort_wgs = (int32_t)((p.n + p.per_wg - 1) / p.per_wg);
+        const dim3 grid((uint32_t)p.sort_wgs);
         int from = -1;
         for (int q = 0; q < passes; ++q) {
             const int to = q & 1;
-            hipLaunchKernelGGL(count_kernel, dim3((uint32_t)p.sort_wgs + (q == 0 ? (uint32_t)fill : 0u)), dim3(SORT_T), 0,
-                               stream, p, from, q * p.bits);
-            hipLaunchKernelGGL(scatter_kernel, dim3((uint32_t)p.sort_wgs), dim3(SORT_T), 0, stream, p, from, to, q * p.bits);
+            hipLaunchKernelGGL(count_kernel, grid, dim3(SORT_T), 0, stream, p, from, q * p.bits);
+            hipLaunchKernelGGL(scatter_kernel, grid, dim3(SORT_T), 0, stream, p, from, to, q * p.bits);
             from = to;
         }
         sorted = from;
     }
-    hipLaunchKernelGGL(sum_kernel<E>, dim3(L.n_shares, slabs), dim3(64), 0, stream, p, sorted);
-    hipLaunchKernelGGL(join_kernel, dim3(JOIN_GRID), dim3(64 * JOIN_W), 0, stream, p, sorted);
+    hipLaunchKernelGGL((sum_kernel<E, ADD>), dim3(L.n_shares + p.fills, columns), dim3(64 * waves), 0, stream, p, sorted);
+    hipLaunchKernelGGL(join_kernel<ADD>, dim3(JOIN_GRID), dim3(64 * JOIN_W), 0, stream, p, sorted);
+}
+
+template <typename E>
+void launch_gradient(GradParams& p, const GradLayout& L, bool add, hipStream_t stream)
+{
+    if (add) launch_gradient<E, true>(p, L, stream);
+    else launch_gradient<E, false>(p, L, stream);
 }
 
 bool misaligned(const void* p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) != 0; }
@@ -654,6 +775,7 @@ int gravac_embedding_lookup(const void* table, int table_type, int64_t vocab, in
     p.table = table; p.tokens = tokens; p.out = out;
     p.vocab = vocab; p.table_stride = table_stride; p.n = n_tokens; p.out_stride = out_stride;
     p.dim = (int32_t)dim; p.wide = token_bytes == 8; p.lanes = 0; p.scale = scale;
+    p.stream = n_tokens * dim * size_of(out_type) > STREAM_BYTES;
     hipStream_t stream = (hipStream_t)stream_v;
     if (table_type == GRAVAC_FLOAT32) launch_lookup<F32>(p, out_type, stream);
     else if (table_type == GRAVAC_BFLOAT16) launch_lookup<BF16>(p, out_type, stream);
@@ -690,17 +812,18 @@ int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tok
     p.n = n_tokens; p.grad_stride = grad_stride; p.table_stride = table_stride;
     p.vocab = vocab; p.padding = padding_token;
     p.dim = (int32_t)dim; p.wide = token_bytes == 8;
-    p.accumulate = (flags & GRAVAC_FLAG_ACCUMULATE) ? 1 : 0;
+    const bool add = (flags & GRAVAC_FLAG_ACCUMULATE) != 0;
     p.scale = scale;
     p.pairs[0] = (uint2*)(ws + L.pairs[0]); p.pairs[1] = (uint2*)(ws + L.pairs[1]);
     p.counts = (uint32_t*)(ws + L.counts); p.joins = (uint32_t*)(ws + L.joins);
     p.head = (float*)(ws + L.head); p.tail = (float*)(ws + L.tail);
     p.part_stride = L.part_stride; p.share_log = L.share_log; p.n_shares = L.n_shares;
-    p.per_wg = 0; p.sort_wgs = 0; p.bits = 0;
+    p.per_wg = 0; p.sort_wgs = 0; p.bits = 0; p.fill_rows = 0; p.fill_wgs = 0; p.fills = 0;
+    p.stream = !add && 4 * vocab * dim > STREAM_BYTES;
     hipStream_t stream = (hipStream_t)stream_v;
-    if (grad_type == GRAVAC_FLOAT32) launch_gradient<F32>(p, L, stream);
-    else if (grad_type == GRAVAC_BFLOAT16) launch_gradient<BF16>(p, L, stream);
-    else launch_gradient<F16>(p, L, stream);
+    if (grad_type == GRAVAC_FLOAT32) launch_gradient<F32>(p, L, add, stream);
+    else if (grad_type == GRAVAC_BFLOAT16) launch_gradient<BF16>(p, L, add, stream);
+    else launch_gradient<F16>(p, L, add, stream);
     return hipGetLastError() == hipSuccess ? GRAVAC_OK : GRAVAC_ERR_HIP;
 }
 
