@@ -41,7 +41,7 @@ constexpr int SLAB = 64;           // bytes of an operand's row that are fetched
 constexpr int BLOCK = 128;         // rows whose slabs stand together in memory
 constexpr int MAX_MAT = GRAVAC_MAX_MATRICES;
 constexpr int MAX_PARTS = 1024;    // partial sums of a matrix's norm at most
-constexpr int PART = 16384;        // elements of one
+constexpr int PART = 4096;         // elements of one, at least
 constexpr int PER_INIT = 48;       // matrices of one launch of the table kernel (its argument holds them)
 constexpr int CUT = 64;            // side of a tile of the kernel that cuts a matrix into operands
 
@@ -62,7 +62,7 @@ struct Mat {     // ... and what the kernels read
     uint32_t cut, part, parts;
     float scale;
     float sx, sa, sq;                 // powers of two: X, E and Q are stored multiplied by them
-    int64_t x, xt[2], lo, e, q, da, dq;   // byte offsets in the workspace
+    int64_t x, xt0, xt1, lo, e, q, da, dq;   // byte offsets in the workspace
 };
 
 struct Tile { uint32_t mat; uint16_t i, j; };
@@ -88,8 +88,8 @@ __host__ __device__ inline int64_t lay_out(Mat& d, int64_t rows, int64_t cols, i
     const int64_t el = split ? 4 : 2, xb = aligned(el * d.mp * d.np), ab = aligned(el * d.mp * d.mp);
     int64_t at = base;
     d.x = at; at += xb;
-    d.xt[0] = at; at += xb;
-    d.xt[1] = at; at += xb;
+    d.xt0 = at; at += xb;
+    d.xt1 = at; at += xb;
     d.lo = at; at += split ? 0 : xb;
     d.e = at; at += ab;
     d.q = at; at += ab;
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256) void cut_kernel(Call p)
         buf[r][c] = x;
     }
     __syncthreads();
-    _Float16 *x = (_Float16*)(p.ws + d.x), *xt = (_Float16*)(p.ws + d.xt[0]), *lo = (_Float16*)(p.ws + d.lo);
+    _Float16 *x = (_Float16*)(p.ws + d.x), *xt = (_Float16*)(p.ws + d.xt0), *lo = (_Float16*)(p.ws + d.lo);
     for (int e = threadIdx.x; e < 2 * CUT * CUT / 8; e += 256) {
         const bool second = e >= CUT * CUT / 8;                    // X^T
         const int row = (e & (CUT * CUT / 8 - 1)) / (CUT / 8), k = (e % (CUT / 8)) * 8;
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
     const Mat d = uniform(p.mats[t.mat]);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int mp = d.mp, width = PRODUCT == GRAM ? d.np : mp;   // length of the sums
-    const int64_t left = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : d.xt[p.flip];
+    const int64_t left = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : p.flip ? d.xt1 : d.xt0;
     const int64_t right = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : d.q;
     const int slabs = width / (SPLIT ? 16 : 32);
 
@@ -457,7 +457,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
                     if (SPLIT) ml[it] = *(const half8*)(e + at + LOW);
                 }
             } else if (PRODUCT == NEXT || PRODUCT == LAST) {
-                const _Float16* xt = (const _Float16*)(ws + (p.flip ? d.xt[1] : d.xt[0]));
+                const _Float16* xt = (const _Float16*)(ws + (p.flip ? d.xt1 : d.xt0));
                 const float* dq = (const float*)(ws + d.dq);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) mj[q] = p.a + dq[j + q];
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
                 }
                 if (PRODUCT != LAST) {
                     cut_8(v, h, l);
-                    _Float16* to = (_Float16*)(ws + (PRODUCT == GRAM ? d.e : PRODUCT == POLY ? d.q : p.flip ? d.xt[0] : d.xt[1]));
+                    _Float16* to = (_Float16*)(ws + (PRODUCT == GRAM ? d.e : PRODUCT == POLY ? d.q : p.flip ? d.xt0 : d.xt1));
                     *(half8*)(to + at) = h;
                     if (SPLIT) *(half8*)(to + at + LOW) = l;
                     else if (PRODUCT == NEXT) *(half8*)((_Float16*)(ws + d.lo) + at) = l;
