@@ -66,6 +66,13 @@ struct Mat {     // ... and what the kernels read
 };
 
 struct Tile { uint32_t mat; uint16_t i, j; };
+constexpr uint32_t NO_MAT = 0xFFFFFFFFu;
+
+// Workgroups go to the eight dies, each with an L2 of its own, in turn.  A product's tiles are listed matrix by matrix, and
+// each die gets one stretch of the list, of about an eighth of the work: its tiles share their operands' rows.  A table has
+// room for the longest stretch on every die.
+constexpr int DIES = 8;
+struct Stretches { uint32_t begin[DIES + 1], longest; };
 
 __host__ __device__ inline int64_t padded(int64_t x, int tile) { return (x + tile - 1) / tile * tile; }
 __host__ __device__ inline int64_t aligned(int64_t x) { return (x + 255) & ~(int64_t)255; }
@@ -126,23 +133,20 @@ struct Call {
 
 struct InitArgs {
     int32_t n, first, split, tile;
+    Stretches list[3];
     MatIn mat[PER_INIT];
 };
 static_assert(sizeof(InitArgs) + sizeof(Call) <= 4096 - 64, "kernel arguments");
 
-// Workgroups go to the eight dies (each with an L2 of its own) in turn.  Where tile number `at` of a matrix's `n` stands among
-// its n slots: each die gets a run of the list, whose tiles lie together in the matrix and share their operands' rows.
-// (`at` counted without regard to the dies: 4096 x 4096 in bfloat16 2.34 instead of 2.07 ms.)
-constexpr uint32_t DIES = 8;
-
-__device__ inline uint32_t slot_of(uint32_t at, uint32_t n)
+__device__ inline uint32_t slot_of(const Stretches& s, uint32_t at)
 {
-    const uint32_t each = n / DIES, more = n % DIES, longer = more * (each + 1);   // `more` dies get one more than the others
-    if (at < longer) return at % (each + 1) * DIES + at / (each + 1);
-    return (at - longer) % each * DIES + more + (at - longer) / each;
+    int die = 0;
+    while (die + 1 < DIES && at >= s.begin[die + 1]) ++die;
+    return (at - s.begin[die]) * DIES + die;
 }
 
-// A matrix's tiles are listed in bands of BAND rows, column by column, so that a run is about as high as it is wide.
+// A matrix's tiles are listed in bands of BAND rows, column by column, so that those next to each other in the list lie in
+// a block about as high as it is wide.
 constexpr uint32_t BAND = 8;
 
 __device__ inline uint32_t place_in_triangle(uint32_t r, uint32_t c, uint32_t n)   // c <= r < n
@@ -173,17 +177,22 @@ __global__ __launch_bounds__(256) void table_kernel(Call p, InitArgs a)
         const uint32_t r = i / tm, c = i % tm;
         if (c > r) continue;
         const Tile t = {id, (uint16_t)r, (uint16_t)c};
-        const uint32_t at = slot_of(place_in_triangle(r, c, tm), tm * (tm + 1) / 2);
-        p.tiles[0][g.tile[0] + at] = t;
-        p.tiles[1][g.tile[1] + at] = t;
+        const uint32_t at = place_in_triangle(r, c, tm);
+        p.tiles[0][slot_of(a.list[0], g.tile[0] + at)] = t;
+        p.tiles[1][slot_of(a.list[1], g.tile[1] + at)] = t;
     }
     for (uint32_t i = threadIdx.x; i < tn * tm; i += 256) {
         const uint32_t r = i / tm, c = i % tm;
-        p.tiles[2][g.tile[2] + slot_of(place_in_square(r, c, tn, tm), tn * tm)] = {id, (uint16_t)r, (uint16_t)c};
+        p.tiles[2][slot_of(a.list[2], g.tile[2] + place_in_square(r, c, tn, tm))] = {id, (uint16_t)r, (uint16_t)c};
     }
     const uint32_t cuts = (uint32_t)(d.mp / CUT) * (uint32_t)(d.np / CUT);
     for (uint32_t i = threadIdx.x; i < cuts; i += 256) p.cut_of[g.cut + i] = id;
     for (uint32_t i = threadIdx.x; i < g.parts; i += 256) p.part_of[g.part + i] = id;
+    if (id == 0)   // the slots behind the shorter stretches
+        for (int k = 0; k < 3; ++k)
+            for (int die = 0; die < DIES; ++die)
+                for (uint32_t i = a.list[k].begin[die + 1] - a.list[k].begin[die] + threadIdx.x; i < a.list[k].longest; i += 256)
+                    p.tiles[k][i * DIES + die] = {NO_MAT, 0, 0};
 }
 
 // The sum over the workgroup's 256 threads, the same for all of them.
@@ -346,6 +355,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
     constexpr int SLABS_BYTES = BUFFERS * 2 * T * SLAB, EPILOGUE_BYTES = 4 * SIDE * PITCH * 4;
     __shared__ __attribute__((aligned(1024))) char lds[SLABS_BYTES > EPILOGUE_BYTES ? SLABS_BYTES : EPILOGUE_BYTES];
     const Tile t = uniform(p.tiles[PRODUCT == GRAM ? 0 : PRODUCT == POLY ? 1 : 2][blockIdx.x]);
+    if (t.mat == NO_MAT) return;
     const Mat d = uniform(p.mats[t.mat]);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int mp = d.mp, width = PRODUCT == GRAM ? d.np : mp;   // length of the sums
@@ -586,7 +596,9 @@ constexpr uint64_t MAX_TILES = 1u << 24;
 
 struct Layout {
     int tile;            // side of a tile
-    uint64_t tiles[3], cuts, parts;
+    Stretches list[3];   // of the products' tiles
+    uint32_t first[3][MAX_MAT];   // a matrix's first tile in them
+    uint64_t cuts, parts;
     int64_t mats, tile_at[3], part_sums, cut_of, part_of, data, total;
 };
 
@@ -616,10 +628,50 @@ int tile_of(const int64_t* matrices, int n_mat)
     return cost[1] < cost[0] ? 256 : 128;
 }
 
+int64_t small_side(const int64_t* matrix) { return std::min(matrix[1], matrix[2]); }
+int64_t large_side(const int64_t* matrix) { return std::max(matrix[1], matrix[2]); }
+
+// The list of a product's tiles (0: A, 1: P, 2: X) and its stretches; false if there are too many.  Long sums come first: their
+// tiles take longest, and a die that has several lengths fills the gaps at the end with short ones.
+bool list_tiles(const int64_t* matrices, int n_mat, int k, Layout& L)
+{
+    uint16_t order[MAX_MAT];
+    for (int i = 0; i < n_mat; ++i) order[i] = (uint16_t)i;
+    auto length = [&](int i) { return k == 0 ? large_side(matrices + 4 * i) : small_side(matrices + 4 * i); };
+    std::sort(order, order + n_mat, [&](int a, int b) { return length(a) != length(b) ? length(a) > length(b) : a < b; });
+    auto tiles = [&](int i) {
+        const uint64_t m = (uint64_t)(padded(small_side(matrices + 4 * i), L.tile) / L.tile);
+        return k < 2 ? m * (m + 1) / 2 : m * (uint64_t)(padded(large_side(matrices + 4 * i), L.tile) / L.tile);
+    };
+    auto work = [&](int i) { return (double)(length(i) + 256); };   // of a tile: its sum, and its begin and end
+    uint64_t count = 0;
+    double all = 0.0;
+    for (int q = 0; q < n_mat; ++q) {
+        L.first[k][order[q]] = (uint32_t)count;
+        count += tiles(order[q]);
+        all += (double)tiles(order[q]) * work(order[q]);
+        if (count > MAX_TILES) return false;
+    }
+    Stretches& s = L.list[k];
+    s.begin[0] = 0;
+    int die = 1;
+    double done = 0.0;
+    for (int q = 0; q < n_mat; ++q) {
+        const double here = (double)tiles(order[q]) * work(order[q]);
+        for (; die < DIES && done + here >= all * die / DIES; ++die)
+            s.begin[die] = L.first[k][order[q]] + (uint32_t)std::min((double)tiles(order[q]), std::round((all * die / DIES - done) / work(order[q])));
+        done += here;
+    }
+    for (; die <= DIES; ++die) s.begin[die] = (uint32_t)count;
+    s.longest = 0;
+    for (int d = 0; d < DIES; ++d) s.longest = std::max(s.longest, s.begin[d + 1] - s.begin[d]);
+    return s.longest <= MAX_TILES / DIES;
+}
+
 // matrices: {offset, rows, cols, stride} each.
 bool lay_out_all(const int64_t* matrices, int n_mat, bool split, Layout& L)
 {
-    std::memset(&L, 0, sizeof(L));
+    L.cuts = L.parts = 0;
     int64_t data = 0;
     for (int i = 0; i < n_mat; ++i) {
         const int64_t rows = matrices[4 * i + 1], cols = matrices[4 * i + 2], stride = matrices[4 * i + 3];
@@ -627,19 +679,19 @@ bool lay_out_all(const int64_t* matrices, int n_mat, bool split, Layout& L)
         if (rows > MAX_SMALL_SIDE && cols > MAX_SMALL_SIDE) return false;
     }
     L.tile = tile_of(matrices, n_mat);
+    for (int k = 0; k < 3; ++k)
+        if (!list_tiles(matrices, n_mat, k, L)) return false;
     for (int i = 0; i < n_mat; ++i) {
         Mat d;
         data += lay_out(d, matrices[4 * i + 1], matrices[4 * i + 2], 0, split, L.tile);
-        const uint64_t tm = d.mp / L.tile, tn = d.np / L.tile;
-        L.tiles[0] += tm * (tm + 1) / 2; L.tiles[1] += tm * (tm + 1) / 2; L.tiles[2] += tm * tn;
         L.cuts += (uint64_t)(d.mp / CUT) * (uint64_t)(d.np / CUT);
         L.parts += parts_of(matrices[4 * i + 1], matrices[4 * i + 2]);
-        if (L.tiles[0] > MAX_TILES || L.tiles[2] > MAX_TILES || L.cuts > MAX_TILES) return false;
+        if (L.cuts > MAX_TILES) return false;
     }
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t here = at; at += aligned(bytes); return here; };
     L.mats = take(sizeof(Mat) * (int64_t)n_mat);
-    for (int k = 0; k < 3; ++k) L.tile_at[k] = take(sizeof(Tile) * (int64_t)L.tiles[k]);
+    for (int k = 0; k < 3; ++k) L.tile_at[k] = take(sizeof(Tile) * DIES * (int64_t)L.list[k].longest);
     L.part_sums = take(8 * (int64_t)L.parts);
     L.cut_of = take(4 * (int64_t)L.cuts);
     L.part_of = take(4 * (int64_t)L.parts);
@@ -712,7 +764,7 @@ void launch_products(Call& p, const Layout& L, int steps, const double* coeffici
     // tiles of 128: two workgroups on a compute unit, one of which multiplies while the other starts or ends; the product with
     // the longest sums has few tiles and takes one workgroup with twice the slabs under way (four 2600 x 650, ResNet101 shape:
     // 140 -> 97 us of it)
-    const dim3 grid[3] = {(uint32_t)L.tiles[0], (uint32_t)L.tiles[1], (uint32_t)L.tiles[2]};
+    const dim3 grid[3] = {DIES * L.list[0].longest, DIES * L.list[1].longest, DIES * L.list[2].longest};
     for (int k = 0; k < steps; ++k) {
         const double* c = coefficients ? coefficients + 3 * k : QUINTIC;
         p.a = (float)c[0]; p.b = (float)c[1]; p.c = (float)c[2];
@@ -730,33 +782,19 @@ template <typename E, bool UPDATE, bool SPLIT>
 int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, int n_mat, int steps, const double* coefficients,
         hipStream_t stream)
 {
-    // long sums first: their tiles take longest, and short ones fill the gaps at the end
-    uint16_t by_m[MAX_MAT], by_n[MAX_MAT];
-    for (int i = 0; i < n_mat; ++i) by_m[i] = by_n[i] = (uint16_t)i;
-    auto small = [&](int i) { return std::min(matrices[4 * i + 1], matrices[4 * i + 2]); };
-    auto large = [&](int i) { return std::max(matrices[4 * i + 1], matrices[4 * i + 2]); };
-    std::sort(by_m, by_m + n_mat, [&](int a, int b) { return small(a) != small(b) ? small(a) > small(b) : a < b; });
-    std::sort(by_n, by_n + n_mat, [&](int a, int b) { return large(a) != large(b) ? large(a) > large(b) : a < b; });
-    uint32_t tile[3][MAX_MAT], at[3] = {0, 0, 0};
-    for (int q = 0; q < n_mat; ++q) {
-        const uint32_t n0 = (uint32_t)(padded(small(by_n[q]), L.tile) / L.tile);
-        tile[0][by_n[q]] = at[0]; at[0] += n0 * (n0 + 1) / 2;
-        const uint32_t m0 = (uint32_t)(padded(small(by_m[q]), L.tile) / L.tile), m1 = (uint32_t)(padded(large(by_m[q]), L.tile) / L.tile);
-        tile[1][by_m[q]] = at[1]; at[1] += m0 * (m0 + 1) / 2;
-        tile[2][by_m[q]] = at[2]; at[2] += m0 * m1;
-    }
     int64_t base = L.data;
     uint32_t cut = 0, part = 0;
     for (int first = 0; first < n_mat; first += PER_INIT) {
         InitArgs a;
         std::memset(&a, 0, sizeof(a));
         a.first = first; a.n = std::min(PER_INIT, n_mat - first); a.split = SPLIT; a.tile = L.tile;
+        for (int s = 0; s < 3; ++s) a.list[s] = L.list[s];
         for (int k = 0; k < a.n; ++k) {
             const int i = first + k;
             MatIn& g = a.mat[k];
             g.offset = matrices[4 * i]; g.rows = (int32_t)matrices[4 * i + 1]; g.cols = (int32_t)matrices[4 * i + 2];
             g.stride = matrices[4 * i + 3];
-            for (int s = 0; s < 3; ++s) g.tile[s] = tile[s][i];
+            for (int s = 0; s < 3; ++s) g.tile[s] = L.first[s][i];
             Mat d;
             g.base = base; base += lay_out(d, g.rows, g.cols, base, SPLIT, L.tile);
             g.cut = cut; cut += (uint32_t)(d.mp / CUT) * (uint32_t)(d.np / CUT);
