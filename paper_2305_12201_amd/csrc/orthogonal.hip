@@ -205,13 +205,22 @@ __device__ double sum_256(double x, double* lds)
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// The matrix's entry that is orthogonalised.  UPDATE: along the momentum (or along the gradient and the momentum).
+// Up to four consecutive entries of what is orthogonalised (n of them; the rest is 0).  UPDATE: the momentum, or the gradient
+// and the momentum.
 template <typename E, bool UPDATE>
-__device__ __forceinline__ float entry(const Call& p, int64_t at)
+__device__ __forceinline__ void entries(const Call& p, int64_t at, int n, float (&x)[4])
 {
-    if (!UPDATE) return to_float<E>(((const typename E::word*)p.in)[at]);
-    const float m = p.momentum[at];
-    return p.nesterov ? p.grad[at] + p.beta * m : m;
+    if (!UPDATE) {
+        load_part<E, 4>((const typename E::word*)p.in + at, n, x);
+        return;
+    }
+    load_part<F32, 4>((const uint32_t*)p.momentum + at, n, x);
+    if (p.nesterov) {
+        float g[4];
+        load_part<F32, 4>((const uint32_t*)p.grad + at, n, g);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] = g[q] + p.beta * x[q];
+    }
 }
 
 // Squares of a share of a matrix's entries, in binary64: no entry is too large or too small for them.  UPDATE: the momentum
@@ -222,16 +231,31 @@ __global__ __launch_bounds__(256) void norm_kernel(Call p)
     __shared__ double lds[4];
     const Mat& d = p.mats[p.part_of[blockIdx.x]];
     const uint32_t part = blockIdx.x - d.part;
-    const int64_t n = (int64_t)d.rows * d.cols;
+    // rows that lie one behind the other are one long row
+    const bool whole = d.stride == d.cols;
+    const int64_t length = whole ? (int64_t)d.rows * d.cols : d.cols, pieces = (length + 3) / 4;   // of four entries, per row
+    const int64_t n = whole ? pieces : pieces * d.rows;
     const int64_t share = (n + d.parts - 1) / d.parts, begin = part * share, end = begin + share < n ? begin + share : n;
     double sum = 0.0;
     for (int64_t i = begin + threadIdx.x; i < end; i += 256) {
-        int64_t at = i;
-        if (d.stride != d.cols) at = i / d.cols * d.stride + i % d.cols;
-        at += d.offset;
-        if (UPDATE) p.momentum[at] = p.beta * p.momentum[at] + p.grad[at];
-        const double x = (double)entry<E, UPDATE>(p, at);
-        sum += x * x;
+        const int64_t row = whole ? 0 : i / pieces, c = (i - row * pieces) * 4, at = d.offset + row * d.stride + c;
+        const int have = length - c < 4 ? (int)(length - c) : 4;
+        float x[4];
+        if (UPDATE) {
+            float g[4];
+            load_part<F32, 4>((const uint32_t*)p.momentum + at, have, x);
+            load_part<F32, 4>((const uint32_t*)p.grad + at, have, g);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = p.beta * x[q] + g[q];
+            store_part<F32, 4>((uint32_t*)p.momentum + at, have, x);
+            if (p.nesterov)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] = g[q] + p.beta * x[q];
+        } else {
+            load_part<E, 4>((const typename E::word*)p.in + at, have, x);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum += (double)x[q] * (double)x[q];
     }
     sum = sum_256(sum, lds);
     if (threadIdx.x == 0) p.parts[blockIdx.x] = sum;
@@ -270,12 +294,14 @@ __global__ __launch_bounds__(256) void cut_kernel(Call p)
     const int across = d.np / CUT;
     const int i0 = (int)(local / across) * CUT, j0 = (int)(local % across) * CUT;   // in X
     const int r0 = d.tall ? j0 : i0, c0 = d.tall ? i0 : j0;                         // in the matrix
-    for (int e = threadIdx.x; e < CUT * CUT; e += 256) {
-        const int r = e / CUT, c = e % CUT;
-        float x = 0.0f;
+#pragma unroll
+    for (int k = 0; k < CUT * CUT / 1024; ++k) {
+        const int e = k * 1024 + (int)threadIdx.x * 4, r = e / CUT, c = e % CUT;
+        float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (r0 + r < d.rows && c0 + c < d.cols)
-            x = (float)((double)entry<E, UPDATE>(p, d.offset + (int64_t)(r0 + r) * d.stride + c0 + c) * inv);
-        buf[r][c] = x;
+            entries<E, UPDATE>(p, d.offset + (int64_t)(r0 + r) * d.stride + c0 + c, d.cols - c0 - c, x);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) buf[r][c + q] = (float)((double)x[q] * inv);
     }
     __syncthreads();
     _Float16 *x = (_Float16*)(p.ws + d.x), *xt = (_Float16*)(p.ws + d.xt0), *lo = (_Float16*)(p.ws + d.lo);
@@ -621,28 +647,27 @@ int parts_of(int64_t rows, int64_t cols)
     return (int)(n < MAX_PARTS ? n : MAX_PARTS);
 }
 
-// Side of the products' tiles.  Tiles of 256 feed the matrix cores with half the LDS traffic of those of 128, but there are a
-// quarter as many and more of them is padding.
-int tile_of(const int64_t* matrices, int n_mat)
-{
-    double cost[2];
-    for (int k = 0; k < 2; ++k) {
-        const int tile = k ? 256 : 128;
-        double work = 0.0, longest = 0.0;   // of the product with X, in units of a tile of 128 and 128 elements of its sum
-        for (int i = 0; i < n_mat; ++i) {
-            const double m = (double)padded(std::min(matrices[4 * i + 1], matrices[4 * i + 2]), tile) / 128.0;
-            const double n = (double)padded(std::max(matrices[4 * i + 1], matrices[4 * i + 2]), tile) / 128.0;
-            const double one = (k ? 4.0 : 1.5);   // time of a tile of this size
-            work += n * m * m * (k ? 1.0 : 1.5) * 1.5;
-            longest = std::max(longest, n * one);
-        }
-        cost[k] = std::max(work / 256.0, longest);
-    }
-    return cost[1] < cost[0] ? 256 : 128;
-}
-
 int64_t small_side(const int64_t* matrix) { return std::min(matrix[1], matrix[2]); }
 int64_t large_side(const int64_t* matrix) { return std::max(matrix[1], matrix[2]); }
+
+// Side of the products' tiles.  Tiles of 256 need half the LDS traffic, but there are a quarter as many and more of them is
+// padding: they pay where A has tiles for half of the compute units, from matrices of four or more a side that are most of the
+// work.  Measured in us with tiles of 128 and of 256, five steps in float32 / bfloat16: 2560 x 5120 1857 and 2831 /
+// 832 and 1183 (55 tiles of A), twelve 1024 x 1024 999 and 1214 / 579 and 615 (120), four 2048 x 2048 2269 and 2318 /
+// 1027 and 1011 (144), 4096 x 4096 4119 and 4064 / 1738 and 1636 (136), twelve 1500 x 3000 4881 and 4722 / 2395 and 2213 (252).
+int tile_of(const int64_t* matrices, int n_mat)
+{
+    double all = 0.0, large = 0.0, tiles = 0.0;
+    for (int i = 0; i < n_mat; ++i) {
+        const int64_t *matrix = matrices + 4 * i;
+        const double m = (double)small_side(matrix), n = (double)large_side(matrix), side = std::ceil(m / 256);
+        all += m * m * n;
+        if (side < 4) continue;
+        large += m * m * n;
+        tiles += side * (side + 1) / 2;
+    }
+    return tiles >= 128 && large >= 0.75 * all ? 256 : 128;
+}
 
 // The list of a product's tiles (0: A, 1: P, 2: X) and its stretches; false if there are too many.  Long sums come first: their
 // tiles take longest, and a die that has several lengths fills the gaps at the end with short ones.
