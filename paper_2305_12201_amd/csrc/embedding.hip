@@ -114,6 +114,7 @@ constexpr int BINS = 1 << MAX_BITS;
 constexpr int SORT_GRID = 128;                   // sorting workgroups at most: each adds up all workgroups' counts
 constexpr int FEW = 1024;                        // calls of at most this many tokens are not sorted
 constexpr int FEW_T = 256, FEW_W = FEW_T / 64;
+constexpr uint32_t FILL_GRID = 1 << 23;          // ... of its workgroups that clear rows at most (the global size has 32 bits)
 
 struct GradParams {
     const void* grad;
@@ -589,17 +590,18 @@ __global__ __launch_bounds__(FEW_T) void sum_few_kernel(GradParams p)
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const uint32_t none = (uint32_t)p.vocab;
     if (blockIdx.x < p.fills) {
-        const uint32_t id = blockIdx.x * gridDim.y + blockIdx.y;
-        if (id >= p.fill_wgs) return;
-        if (threadIdx.x < 64) named[threadIdx.x] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < p.n; i += FEW_T) {
-            const uint32_t k = key_at(p, i);
-            if (k != none && k / p.fill_rows == id) named[k % p.fill_rows] = 1;
+        for (uint32_t id = blockIdx.x * gridDim.y + blockIdx.y; id < p.fill_wgs; id += p.fills * gridDim.y) {
+            __syncthreads();
+            if (threadIdx.x < 64) named[threadIdx.x] = 0;
+            __syncthreads();
+            for (int i = threadIdx.x; i < p.n; i += FEW_T) {
+                const uint32_t k = key_at(p, i);
+                if (k != none && k / p.fill_rows == id) named[k % p.fill_rows] = 1;
+            }
+            __syncthreads();
+            const int64_t row0 = (int64_t)id * p.fill_rows;
+            clear_rows(p, row0, __ballot(lane < p.fill_rows && row0 + lane < p.vocab && !named[lane]));
         }
-        __syncthreads();
-        const int64_t row0 = (int64_t)id * p.fill_rows;
-        clear_rows(p, row0, __ballot(lane < p.fill_rows && row0 + lane < p.vocab && !named[lane]));
         return;
     }
     const int groups = (int)((p.n + 63) / 64), t = (int)(blockIdx.x - p.fills);
@@ -714,6 +716,7 @@ void launch_gradient(GradParams& p, const GradLayout& L, hipStream_t stream)
         p.fill_rows = (int32_t)(rows < 1 ? 1 : rows > 64 ? 64 : rows);
         p.fill_wgs = (uint32_t)((p.vocab + p.fill_rows - 1) / p.fill_rows);
         p.fills = (p.fill_wgs + columns - 1) / columns;
+        if (p.n <= FEW && p.fills > FILL_GRID) p.fills = FILL_GRID;
     }
     if (p.n <= FEW) {
         if (p.n + p.fills > 0)

@@ -38,6 +38,8 @@ typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr int SLAB = 64;           // bytes of an operand's row that are fetched at a time: 16 elements as hi and lo, or 32 hi
+constexpr int PART_SLABS = 128;    // slabs of a sum that are added one after the other (tiles of 128)
+constexpr int64_t LONG_SIDE = 32768;   // no tiles of 256 for longer sums
 constexpr int BLOCK = 128;         // rows whose slabs stand together in memory
 constexpr int MAX_MAT = GRAVAC_MAX_MATRICES;
 constexpr int MAX_PARTS = 1024;    // partial sums of a matrix's norm at most
@@ -458,7 +460,23 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
     // busy 61 % of the time).
     constexpr int PRODUCTS = SPLIT ? 3 : 2, INSTS = PRODUCTS * F * F, ITEMS = 6 * F;
     // (sides are padded to 128 elements of two bytes or more: an even number of slabs)
-    for (int s0 = 0; s0 < slabs; s0 += 2)
+    // A long sum is added up in parts: added one after the other, 70,001 elements of float32 are off by 16 times what the
+    // plain evaluation's nested sums are.  (There are no registers for that with tiles of 256, which longer sums do not get.)
+    constexpr bool PARTS = F == 2;
+    float16v sums[PARTS ? F : 1][PARTS ? F : 1];
+    auto add_up = [&](bool first) {
+#pragma unroll
+        for (int i = 0; i < (PARTS ? F : 0); ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    sums[i][j][q] = first ? acc[i][j][q] : sums[i][j][q] + acc[i][j][q];
+                    acc[i][j][q] = 0.0f;
+                }
+    };
+    for (int s0 = 0; s0 < slabs; s0 += 2) {
+        if (PARTS && s0 % PART_SLABS == 0 && s0 > 0) add_up(s0 == PART_SLABS);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int s = s0 + u;
@@ -477,6 +495,14 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+    }
+    if (PARTS && slabs > PART_SLABS) {
+        add_up(false);
+#pragma unroll
+        for (int i = 0; i < (PARTS ? F : 0); ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[i][j] = sums[i][j];
+    }
     arrived<0>();   // nothing more comes, and the LDS of the slabs is free
 
     // A wavefront puts 64 x 64 of its sums at a time into LDS and reads them back eight along the left index at a time, for
@@ -631,7 +657,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
 // ---------------------------------------------------------------------------------------------------------------------
 
 constexpr int64_t MAX_SIDE = 1 << 20, MAX_SMALL_SIDE = 32768, MAX_FLAT = 1LL << 40;
-constexpr uint64_t MAX_TILES = 1u << 24;
+constexpr uint64_t MAX_TILES = (1u << 24) - 8;   // (256 threads each: the grid has 32 bits)
 
 struct Layout {
     int tile;            // side of a tile
@@ -662,6 +688,7 @@ int tile_of(const int64_t* matrices, int n_mat)
         const int64_t *matrix = matrices + 4 * i;
         const double m = (double)small_side(matrix), n = (double)large_side(matrix), side = std::ceil(m / 256);
         all += m * m * n;
+        if (large_side(matrix) > LONG_SIDE) return 128;
         if (side < 4) continue;
         large += m * m * n;
         tiles += side * (side + 1) / 2;
@@ -742,20 +769,19 @@ bool lay_out_all(const int64_t* matrices, int n_mat, bool split, Layout& L)
 bool lie_apart(const int64_t* matrices, int n_mat, int64_t n)
 {
     auto end = [&](int i) { return matrices[4 * i] + (matrices[4 * i + 1] - 1) * matrices[4 * i + 3] + matrices[4 * i + 2]; };
-    bool ascending = true;
+    uint16_t order[MAX_MAT];
     for (int i = 0; i < n_mat; ++i) {
+        order[i] = (uint16_t)i;
         if (matrices[4 * i] < 0 || matrices[4 * i] > n || end(i) > n) return false;
-        if (i > 0 && matrices[4 * i] < end(i - 1)) ascending = false;
     }
-    if (ascending) return true;
+    std::sort(order, order + n_mat, [&](int a, int b) { return matrices[4 * a] < matrices[4 * b]; });
     for (int i = 0; i < n_mat; ++i)
-        for (int k = 0; k < i; ++k) {
-            const int64_t *a = matrices + 4 * i, *b = matrices + 4 * k;
-            if (a[0] >= end(k) || b[0] >= end(i)) continue;
+        for (int k = i + 1; k < n_mat && matrices[4 * order[k]] < end(order[i]); ++k) {
             // spans that overlap: only columns of one larger matrix lie apart (equal strides, and no columns in common)
+            const int64_t *a = matrices + 4 * order[i], *b = matrices + 4 * order[k];
             if (a[3] != b[3]) return false;
-            const int64_t s = a[3], d = ((b[0] - a[0]) % s + s) % s;   // b's first column, counted from a's
-            if (d < a[2] || d + b[2] > s) return false;
+            const int64_t d = (b[0] - a[0]) % a[3];   // b's first column, counted from a's
+            if (d < a[2] || d + b[2] > a[3]) return false;
         }
     return true;
 }

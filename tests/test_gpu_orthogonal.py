@@ -106,6 +106,36 @@ def test_orthogonalize(rows, cols, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(3, 70_001), (40_003, 20), (1, 300_000), (130, 20_000)])
+def test_long_matrices(rows, cols, dtype):
+    G = _values(rows, cols, "normal", 17).to(dtype)
+    got = _orthogonalize(G.cuda().view(-1), [(0, rows, cols)]).cpu().view(rows, cols)
+    assert _error(got, _exact(G)) <= _tolerance(G, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_matrices(dtype):
+    """A call large enough for the larger tiles, some of its matrices small and ragged; 64 bits on the GPU."""
+    shapes = [(2048, 2111), (2100, 2048), (2048, 2048), (3000, 2050), (70, 130), (1, 9)]
+    at, matrices = 1, []
+    for r, c in shapes:
+        matrices.append((at, r, c))
+        at += r * c + 3
+    g = torch.Generator(device="cuda").manual_seed(18)
+    x = (torch.randn(at, device="cuda", generator=g)).to(dtype)
+    got = _orthogonalize(x, matrices)
+    for off, r, c in matrices:
+        G = x[off:off + r * c].view(r, c)
+        want = _exact(G)
+        if dtype != torch.bfloat16:
+            # (the binary32 evaluation that _tolerance compares with, on the GPU as well)
+            bound = 12 * _error(_exact(G, dtype=torch.float32), want) + 2.0 ** -22 + (HALF_STEP[dtype] if dtype == torch.float16 else 0.0)
+        else:
+            bound = 2 * _error(_rounded_operands(G), want) + HALF_STEP[dtype]
+        assert _error(got[off:off + r * c].view(r, c), want) <= bound, (r, c)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("steps,coefficients", [(1, QUINTIC), (2, CUBIC), (12, CUBIC), (8, (15 / 8, -10 / 8, 3 / 8))])
 def test_other_steps_and_coefficients(dtype, steps, coefficients):
     G = _values(96, 200, "normal", 5).to(dtype)
