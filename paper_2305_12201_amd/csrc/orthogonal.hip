@@ -94,11 +94,13 @@ __host__ __device__ inline int64_t lay_out(Mat& d, int64_t rows, int64_t cols, i
     d.tall = rows > cols;
     d.m = (int32_t)(d.tall ? cols : rows); d.n = (int32_t)(d.tall ? rows : cols);
     d.mp = (int32_t)padded(d.m, tile); d.np = (int32_t)padded(d.n, tile);
-    const int64_t el = split ? 4 : 2, xb = aligned(el * d.mp * d.np), ab = aligned(el * d.mp * d.mp);
+    // (the rows of an operand stand in blocks)
+    const int64_t el = split ? 4 : 2, mb = padded(d.mp, BLOCK), nb = padded(d.np, BLOCK);
+    const int64_t xb = aligned(el * mb * d.np), tb = aligned(el * nb * d.mp), ab = aligned(el * mb * d.mp);
     int64_t at = base;
     d.x = at; at += xb;
-    d.xt0 = at; at += xb;
-    d.xt1 = at; at += xb;
+    d.xt0 = at; at += tb;
+    d.xt1 = at; at += tb;
     d.lo = at; at += split ? 0 : xb;
     d.e = at; at += ab;
     d.q = at; at += ab;
@@ -134,7 +136,7 @@ struct Call {
 // ---------------------------------------------------------------------------------------------------------------------
 
 struct InitArgs {
-    int32_t n, first, split, tile;
+    int32_t n, first, split, tile, side[3];
     Stretches list[3];
     MatIn mat[PER_INIT];
 };
@@ -174,18 +176,14 @@ __global__ __launch_bounds__(256) void table_kernel(Call p, InitArgs a)
     d.offset = g.offset; d.stride = g.stride;
     d.cut = g.cut; d.part = g.part; d.parts = g.parts; d.scale = g.scale;
     if (threadIdx.x == 0) p.mats[id] = d;
-    const uint32_t tm = (uint32_t)(d.mp / a.tile), tn = (uint32_t)(d.np / a.tile);
-    for (uint32_t i = threadIdx.x; i < tm * tm; i += 256) {
-        const uint32_t r = i / tm, c = i % tm;
-        if (c > r) continue;
-        const Tile t = {id, (uint16_t)r, (uint16_t)c};
-        const uint32_t at = place_in_triangle(r, c, tm);
-        p.tiles[0][slot_of(a.list[0], g.tile[0] + at)] = t;
-        p.tiles[1][slot_of(a.list[1], g.tile[1] + at)] = t;
-    }
-    for (uint32_t i = threadIdx.x; i < tn * tm; i += 256) {
-        const uint32_t r = i / tm, c = i % tm;
-        p.tiles[2][slot_of(a.list[2], g.tile[2] + place_in_square(r, c, tn, tm))] = {id, (uint16_t)r, (uint16_t)c};
+    for (int k = 0; k < 3; ++k) {
+        const uint32_t tm = (uint32_t)(d.mp / a.side[k]), tn = k < 2 ? tm : (uint32_t)(d.np / a.side[k]);
+        for (uint32_t i = threadIdx.x; i < tn * tm; i += 256) {
+            const uint32_t r = i / tm, c = i % tm;
+            if (k < 2 && c > r) continue;
+            const uint32_t at = k < 2 ? place_in_triangle(r, c, tm) : place_in_square(r, c, tn, tm);
+            p.tiles[k][slot_of(a.list[k], g.tile[k] + at)] = {id, (uint16_t)r, (uint16_t)c};
+        }
     }
     const uint32_t cuts = (uint32_t)(d.mp / CUT) * (uint32_t)(d.np / CUT);
     for (uint32_t i = threadIdx.x; i < cuts; i += 256) p.cut_of[g.cut + i] = id;
@@ -385,15 +383,15 @@ __device__ __forceinline__ float take_diagonal(float (&v)[8], bool on_diagonal, 
     return x;
 }
 
-// C = L R^T on tiles of 64 F x 64 F, four wavefronts of 32 F x 32 F.  A slab of an operand is 64 F rows of SLAB bytes in LDS;
+// C = L R^T on tiles of 64 F x 64 F (F = 1, 2, 4), four wavefronts of 32 F x 32 F.  A slab of an operand is 64 F rows of SLAB bytes in LDS;
 // the 16-byte chunks of a row are stored in an order turned by the row, so that the lanes that read one chunk of eight
 // consecutive rows touch all banks.  While a slab is multiplied from registers, the next is read from LDS into others and
 // those behind it are on their way from memory, BUFFERS - 2 of them.
 template <Product PRODUCT, bool SPLIT, typename E, bool UPDATE, int F, int BUFFERS>
-__global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_kernel(Call p)
+__global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) void product_kernel(Call p)
 {
     constexpr int T = 64 * F, LOADS = 2 * F;              // a wavefront's loads per slab
-    constexpr int SIDE = 64;                              // the epilogue goes through LDS in blocks of 64 x 64
+    constexpr int SIDE = F == 1 ? 32 : 64;                // the epilogue goes through LDS in blocks of SIDE x SIDE
     constexpr int SLABS_BYTES = BUFFERS * 2 * T * SLAB, EPILOGUE_BYTES = 4 * SIDE * SIDE * 4;
     __shared__ __attribute__((aligned(1024))) char lds[SLABS_BYTES > EPILOGUE_BYTES ? SLABS_BYTES : EPILOGUE_BYTES];
     const Tile t = uniform(p.tiles[PRODUCT == GRAM ? 0 : PRODUCT == POLY ? 1 : 2][blockIdx.x]);
@@ -418,11 +416,11 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
         const uint32_t to = fetch_to + (uint32_t)((slab & (BUFFERS - 1)) * 2 * T * SLAB);
         constexpr int ROWS = 16 * SLAB;
         if (q == 0) fetch_16<0>(from_left + at, fetch_at, to);
-        if (q == 1) fetch_16<ROWS>(from_left + at, fetch_at, to);
+        if (F > 1 && q == 1) fetch_16<ROWS>(from_left + at, fetch_at, to);
         if (F == 4 && q == 2) fetch_16<2 * ROWS>(from_left + at, fetch_at, to);
         if (F == 4 && q == 3) fetch_16<3 * ROWS>(from_left + at, fetch_at, to);
         if (q == F) fetch_16<0>(from_right + at, fetch_at, to + T * SLAB);
-        if (q == F + 1) fetch_16<ROWS>(from_right + at, fetch_at, to + T * SLAB);
+        if (F > 1 && q == F + 1) fetch_16<ROWS>(from_right + at, fetch_at, to + T * SLAB);
         if (F == 4 && q == F + 2) fetch_16<2 * ROWS>(from_right + at, fetch_at, to + T * SLAB);
         if (F == 4 && q == F + 3) fetch_16<3 * ROWS>(from_right + at, fetch_at, to + T * SLAB);
     };
@@ -462,7 +460,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
     // (sides are padded to 128 elements of two bytes or more: an even number of slabs)
     // A long sum is added up in parts: added one after the other, 70,001 elements of float32 are off by 16 times what the
     // plain evaluation's nested sums are.  (There are no registers for that with tiles of 256, which longer sums do not get.)
-    constexpr bool PARTS = F == 2;
+    constexpr bool PARTS = F <= 2;
     float16v sums[PARTS ? F : 1][PARTS ? F : 1];
     auto add_up = [&](bool first) {
 #pragma unroll
@@ -511,16 +509,21 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
     // the matrix instructions leave them, eight rows of a column and eight columns of a row all touch the banks evenly.
     // (Four bytes at a time in rows of 65: 3.4 us of a kernel's 5.8, now PLACE.)
     float* block = (float*)lds + w * SIDE * SIDE;
-    auto spot = [](int i, int j) { return j * SIDE + (((i >> 2) + j + 2 * (j >> 3)) & 15) * 4 + (i & 3); };
+    auto spot = [](int i, int j) { return j * SIDE + (((i >> 2) + j + 2 * (j >> 3)) & (SIDE / 4 - 1)) * 4 + (i & 3); };
+    constexpr int BLOCKS = 32 * F / SIDE, EIGHTS = SIDE / 8, COLUMNS = 64 / EIGHTS;   // lanes: eights of a column, columns
     char* ws = p.ws;
 #pragma unroll
-    for (int bi = 0; bi < F / 2; ++bi)
+    for (int bi = 0; bi < BLOCKS; ++bi)
 #pragma unroll
-        for (int bj = 0; bj < F / 2; ++bj) {
+        for (int bj = 0; bj < BLOCKS; ++bj) {
             const int i0 = t.i * T + wi + bi * SIDE, j0 = t.j * T + wj + bj * SIDE;
-            const int part = (lane & 7) * 8, i = i0 + part;
+            // A symmetric matrix takes its upper half from the lower one, in units of 32 whatever the tiles are: so the result
+            // does not depend on them (the parts of a product are added in another order on the other side).
+            constexpr bool SYMMETRIC = PRODUCT == GRAM || PRODUCT == POLY;
+            if (SYMMETRIC && i0 < j0) continue;
+            const int part = (lane % EIGHTS) * 8, column = lane / EIGHTS, i = i0 + part;
             // what the sums meet in memory, all of it under way before the first is used
-            constexpr int ROWS = SIDE / 8;
+            constexpr int ROWS = SIDE / COLUMNS;
             half8 mh[ROWS], ml[ROWS];
             float mj[ROWS], mi[8];
             if (PRODUCT == POLY) {
@@ -530,7 +533,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
                 for (int q = 0; q < 8; ++q) mi[q] = da[i + q];
 #pragma unroll
                 for (int it = 0; it < ROWS; ++it) {
-                    const int j = j0 + it * 8 + (lane >> 3);
+                    const int j = j0 + it * COLUMNS + column;
                     const int64_t at = place<SPLIT>(j, mp, i);
                     mj[it] = da[j];
                     mh[it] = *(const half8*)(e + at);
@@ -542,7 +545,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
                 const float* dq = (const float*)(ws + d.dq);
 #pragma unroll
                 for (int it = 0; it < ROWS; ++it) {
-                    const int j = j0 + it * 8 + (lane >> 3);
+                    const int j = j0 + it * COLUMNS + column;
                     const int64_t at = place<SPLIT>(j, d.np, i);
                     mj[it] = p.a + dq[j];
                     mh[it] = *(const half8*)(x + at);
@@ -551,23 +554,28 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
             }
             // acc[4 g + q] of lane l is row 8 g + 4 (l / 32) + q, column l % 32 of its 32 x 32
 #pragma unroll
-            for (int ti = 0; ti < 2; ++ti)
+            for (int ti = 0; ti < SIDE / 32; ++ti)
 #pragma unroll
-                for (int tj = 0; tj < 2; ++tj)
+                for (int tj = 0; tj < SIDE / 32; ++tj)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const float16v& v = acc[bi * 2 + ti][bj * 2 + tj];
+                        const float16v& v = acc[bi * (SIDE / 32) + ti][bj * (SIDE / 32) + tj];
+                        if (SYMMETRIC && SIDE > 32 && ti != tj && i0 == j0) {
+                            if (ti < tj) continue;
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) block[spot(tj * 32 + frag_row, ti * 32 + g * 8 + frag_half * 4 + q)] = v[g * 4 + q];
+                        }
                         *(float4*)&block[spot(ti * 32 + g * 8 + frag_half * 4, tj * 32 + frag_row)] =
                             make_float4(v[g * 4], v[g * 4 + 1], v[g * 4 + 2], v[g * 4 + 3]);
                     }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             bool other;   // whether the other orientation is wanted
-            if (PRODUCT == GRAM || PRODUCT == POLY) other = t.i != t.j;
+            if (SYMMETRIC) other = i0 != j0;
             else if (PRODUCT == NEXT) other = true;
             else other = d.tall;
 #pragma unroll
             for (int it = 0; it < ROWS; ++it) {
-                const int jj = it * 8 + (lane >> 3), j = j0 + jj;
+                const int jj = it * COLUMNS + column, j = j0 + jj;
                 float4* mine[2] = {(float4*)&block[spot(part, jj)], (float4*)&block[spot(part + 4, jj)]};
                 const float4 low = *mine[0], high = *mine[1];
                 float v[8] = {low.x, low.y, low.z, low.w, high.x, high.y, high.z, high.w};
@@ -623,7 +631,7 @@ __global__ __launch_bounds__(256, F == 4 || BUFFERS > 4 ? 1 : 2) void product_ke
             if (other) {
 #pragma unroll
                 for (int it = 0; it < ROWS; ++it) {
-                    const int ii = it * 8 + (lane >> 3), i = i0 + ii, j = j0 + part;
+                    const int ii = it * COLUMNS + column, i = i0 + ii, j = j0 + part;
                     float v[8];
 #pragma unroll
                     for (int q = 0; q < 8; ++q) v[q] = block[spot(ii, part + q)];
@@ -660,7 +668,8 @@ constexpr int64_t MAX_SIDE = 1 << 20, MAX_SMALL_SIDE = 32768, MAX_FLAT = 1LL << 
 constexpr uint64_t MAX_TILES = (1u << 24) - 8;   // (256 threads each: the grid has 32 bits)
 
 struct Layout {
-    int tile;            // side of a tile
+    int tile;            // sides are padded to whole tiles of it: the largest of the three
+    int side[3];         // of a tile of A, P and X
     Stretches list[3];   // of the products' tiles
     uint32_t first[3][MAX_MAT];   // a matrix's first tile in them
     uint64_t cuts, parts;
@@ -696,6 +705,41 @@ int tile_of(const int64_t* matrices, int n_mat)
     return tiles >= 128 && large >= 0.75 * all ? 256 : 128;
 }
 
+// A product's tiles (0: A, 1: P, 2: X) if they have this side and sides are padded to `pad`.
+uint64_t tiles_of(const int64_t* matrix, int k, int64_t side, int64_t pad)
+{
+    const uint64_t m = (uint64_t)(padded(small_side(matrix), (int)pad) / side), n = (uint64_t)(padded(large_side(matrix), (int)pad) / side);
+    return k < 2 ? m * (m + 1) / 2 : m * n;
+}
+
+// Tiles of 64 where those of 128 would be few: they bring more compute units to work and their epilogues are short.  us for five
+// steps in float32, with A, P and X in tiles of 128 / A in 64 / A and P / all: 512 x 512 234, 202, 165, 135; 1024 x 1024 344,
+// 297, 241, 197; four 2600 x 650 (84 tiles of 128 of A and P, 504 of X) 548, 492, 465, 542; 1536 x 1536 (78, 144) 464, 438, 398,
+// 418; four 1024 x 1024 (144, 256) 427, 439, 438, 469; the ResNet101 shape (405, 2700) with P alone in 64 1924 -> 1863.
+// Twelve 300 x 900 are 245 with X in 128 and 228 in 64 for the padding alone.
+// P among tiles of 256 takes 128 where a last round of those would leave more units idle: VGG16 shape 22.6 -> 21.9 ms.
+void choose_sides(const int64_t* matrices, int n_mat, Layout& L)
+{
+    const int tile = tile_of(matrices, n_mat);
+    auto count = [&](int k, int side) {
+        double n = 0.0;
+        for (int i = 0; i < n_mat; ++i) n += (double)tiles_of(matrices + 4 * i, k, side, tile == 256 ? 256 : side);
+        return n;
+    };
+    L.tile = tile;
+    L.side[0] = L.side[1] = L.side[2] = tile;
+    if (tile == 256) {
+        auto busy = [](double tiles, double at_once) { return tiles / (at_once * std::ceil(tiles / at_once)); };
+        if (0.93 * busy(count(1, 128), 512.0) > busy(count(1, 256), 256.0)) L.side[1] = 128;
+        return;
+    }
+    const double square = count(0, 128), whole = count(2, 128);
+    if (square <= 128) L.side[0] = 64;
+    if (square <= 512) L.side[1] = 64;
+    if (whole <= 128 || (L.side[0] == 64 && 4.0 * whole > 1.2 * count(2, 64))) L.side[2] = 64;
+    L.tile = std::max(std::max(L.side[0], L.side[1]), L.side[2]);
+}
+
 // The list of a product's tiles (0: A, 1: P, 2: X) and its stretches; false if there are too many.  Long sums come first: their
 // tiles take longest, and a die that has several lengths fills the gaps at the end with short ones.
 bool list_tiles(const int64_t* matrices, int n_mat, int k, Layout& L)
@@ -705,8 +749,7 @@ bool list_tiles(const int64_t* matrices, int n_mat, int k, Layout& L)
     auto length = [&](int i) { return k == 0 ? large_side(matrices + 4 * i) : small_side(matrices + 4 * i); };
     std::sort(order, order + n_mat, [&](int a, int b) { return length(a) != length(b) ? length(a) > length(b) : a < b; });
     auto tiles = [&](int i) {
-        const uint64_t m = (uint64_t)(padded(small_side(matrices + 4 * i), L.tile) / L.tile);
-        return k < 2 ? m * (m + 1) / 2 : m * (uint64_t)(padded(large_side(matrices + 4 * i), L.tile) / L.tile);
+        return tiles_of(matrices + 4 * i, k, L.side[k], L.tile);
     };
     auto work = [&](int i) { return (double)(length(i) + 256); };   // of a tile: its sum, and its begin and end
     uint64_t count = 0;
@@ -743,7 +786,7 @@ bool lay_out_all(const int64_t* matrices, int n_mat, bool split, Layout& L)
         if (rows < 1 || cols < 1 || rows > MAX_SIDE || cols > MAX_SIDE || stride < cols || stride > MAX_FLAT) return false;
         if (rows > MAX_SMALL_SIDE && cols > MAX_SMALL_SIDE) return false;
     }
-    L.tile = tile_of(matrices, n_mat);
+    choose_sides(matrices, n_mat, L);
     for (int k = 0; k < 3; ++k)
         if (!list_tiles(matrices, n_mat, k, L)) return false;
     for (int i = 0; i < n_mat; ++i) {
@@ -822,23 +865,29 @@ bool bounded(const double* coefficients, int steps)
 
 constexpr double QUINTIC[3] = {3.4445, -4.7750, 2.0315};
 
-template <typename E, bool UPDATE, bool SPLIT, int F>
+// Tiles of 128: two workgroups on a compute unit, one of which multiplies while the other starts or ends; A, whose sums are the
+// longest, has fewer tiles and takes one with twice the slabs under way (ResNet101 shape: 140 -> 97 us).
+template <Product PRODUCT, typename E, bool UPDATE, bool SPLIT>
+void launch_product(const Call& p, const Layout& L, hipStream_t stream)
+{
+    constexpr int K = PRODUCT == GRAM ? 0 : PRODUCT == POLY ? 1 : 2;
+    const dim3 grid(DIES * L.list[K].longest);
+    if (L.side[K] == 256) hipLaunchKernelGGL((product_kernel<PRODUCT, SPLIT, E, UPDATE, 4, 4>), grid, dim3(256), 0, stream, p);
+    else if (L.side[K] == 128) hipLaunchKernelGGL((product_kernel<PRODUCT, SPLIT, E, UPDATE, 2, PRODUCT == GRAM ? 8 : 4>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((product_kernel<PRODUCT, SPLIT, E, UPDATE, 1, 8>), grid, dim3(256), 0, stream, p);
+}
+
+template <typename E, bool UPDATE, bool SPLIT>
 void launch_products(Call& p, const Layout& L, int steps, const double* coefficients, hipStream_t stream)
 {
-    // tiles of 128: two workgroups on a compute unit, one of which multiplies while the other starts or ends; the product with
-    // the longest sums has few tiles and takes one workgroup with twice the slabs under way (four 2600 x 650, ResNet101 shape:
-    // 140 -> 97 us of it)
-    const dim3 grid[3] = {DIES * L.list[0].longest, DIES * L.list[1].longest, DIES * L.list[2].longest};
     for (int k = 0; k < steps; ++k) {
         const double* c = coefficients ? coefficients + 3 * k : QUINTIC;
         p.a = (float)c[0]; p.b = (float)c[1]; p.c = (float)c[2];
         p.flip = k & 1;
-        hipLaunchKernelGGL((product_kernel<GRAM, SPLIT, F32, false, F, F == 4 ? 4 : 8>), grid[0], dim3(256), 0, stream, p);
-        hipLaunchKernelGGL((product_kernel<POLY, SPLIT, F32, false, F, 4>), grid[1], dim3(256), 0, stream, p);
-        if (k + 1 < steps)
-            hipLaunchKernelGGL((product_kernel<NEXT, SPLIT, F32, false, F, 4>), grid[2], dim3(256), 0, stream, p);
-        else
-            hipLaunchKernelGGL((product_kernel<LAST, SPLIT, E, UPDATE, F, 4>), grid[2], dim3(256), 0, stream, p);
+        launch_product<GRAM, F32, false, SPLIT>(p, L, stream);
+        launch_product<POLY, F32, false, SPLIT>(p, L, stream);
+        if (k + 1 < steps) launch_product<NEXT, F32, false, SPLIT>(p, L, stream);
+        else launch_product<LAST, E, UPDATE, SPLIT>(p, L, stream);
     }
 }
 
@@ -852,6 +901,7 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
         InitArgs a;
         std::memset(&a, 0, sizeof(a));
         a.first = first; a.n = std::min(PER_INIT, n_mat - first); a.split = SPLIT; a.tile = L.tile;
+        for (int s = 0; s < 3; ++s) a.side[s] = L.side[s];
         for (int s = 0; s < 3; ++s) a.list[s] = L.list[s];
         for (int k = 0; k < a.n; ++k) {
             const int i = first + k;
@@ -869,8 +919,7 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
     }
     hipLaunchKernelGGL((norm_kernel<E, UPDATE>), dim3((uint32_t)L.parts), dim3(256), 0, stream, p);
     hipLaunchKernelGGL((cut_kernel<E, UPDATE, SPLIT>), dim3((uint32_t)L.cuts), dim3(256), 0, stream, p);
-    if (L.tile == 256) launch_products<E, UPDATE, SPLIT, 4>(p, L, steps, coefficients, stream);
-    else launch_products<E, UPDATE, SPLIT, 2>(p, L, steps, coefficients, stream);
+    launch_products<E, UPDATE, SPLIT>(p, L, steps, coefficients, stream);
     return hipGetLastError() == hipSuccess ? GRAVAC_OK : GRAVAC_ERR_HIP;
 }
 
