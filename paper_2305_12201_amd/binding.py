@@ -348,15 +348,17 @@ def _check_device(*tensors) -> None:
     """The library works on the current device: a tensor of another one is refused."""
     here = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != here):
+        if t is not None and t.get_device() != here:
             raise ValueError(f"expected a tensor of the current device cuda:{here}, got {t.device}")
 
 
 def _rows(t, what: str):
-    """(pointer, stride) of a matrix whose rows are consecutive elements."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    """(pointer, rows, columns, stride) of a matrix whose rows are consecutive elements."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{what}: expected a matrix whose rows are consecutive elements")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    rows, cols = shape
+    return t.data_ptr(), rows, cols, stride[0] if rows > 1 else max(stride[0], cols)
 
 
 def _tokens(t):
@@ -379,13 +381,13 @@ def gravac_embedding_lookup(table, tokens, out, *, scale=1.0, stream=None) -> No
     outside the table.  ``table`` and ``out`` are matrices of float32, bfloat16 or float16 whose rows may lie apart;
     ``tokens`` is contiguous int32 or int64 of any shape with as many entries as ``out`` has rows."""
     _check_device(table, tokens, out)
-    tp, ts = _rows(table, "table")
-    op, os_ = _rows(out, "out")
+    tp, vocab, dim, ts = _rows(table, "table")
+    op, rows, cols, os_ = _rows(out, "out")
     kp, kb, n = _tokens(tokens)
-    if out.shape[0] != n or out.shape[1] != table.shape[1]:
-        raise ValueError(f"out: expected {n} rows of {table.shape[1]}, got {tuple(out.shape)}")
-    rc = lib().gravac_embedding_lookup(tp, _type_of(table.dtype), table.shape[0], table.shape[1], ts, kp, kb, n,
-                                       float(scale), op, _type_of(out.dtype), os_, _stream_handle(stream))
+    if rows != n or cols != dim:
+        raise ValueError(f"out: expected {n} rows of {dim}, got {tuple(out.shape)}")
+    rc = lib().gravac_embedding_lookup(tp, _type_of(table.dtype), vocab, dim, ts, kp, kb, n, float(scale), op, _type_of(out.dtype), os_,
+                                       _stream_handle(stream))
     if rc != OK:
         raise GravacError(rc, "gravac_embedding_lookup")
 
@@ -405,16 +407,15 @@ def gravac_embedding_gradient(grad_out, tokens, table_grad, *, scale=1.0, paddin
     it is added to what is there.  ``workspace``: a uint8 device tensor of at least
     ``gravac_embedding_gradient_workspace_bytes`` bytes."""
     _check_device(grad_out, tokens, table_grad, workspace)
-    gp, gs = _rows(grad_out, "grad_out")
-    tp, ts = _rows(table_grad, "table_grad")
+    gp, rows, cols, gs = _rows(grad_out, "grad_out")
+    tp, vocab, dim, ts = _rows(table_grad, "table_grad")
     kp, kb, n = _tokens(tokens)
     if table_grad.dtype != torch.float32:
         raise TypeError(f"table_grad: expected float32, got {table_grad.dtype}")
-    if grad_out.shape[0] != n or grad_out.shape[1] != table_grad.shape[1]:
-        raise ValueError(f"grad_out: expected {n} rows of {table_grad.shape[1]}, got {tuple(grad_out.shape)}")
+    if rows != n or cols != dim:
+        raise ValueError(f"grad_out: expected {n} rows of {dim}, got {tuple(grad_out.shape)}")
     wp, wb = _workspace(workspace)
-    rc = lib().gravac_embedding_gradient(gp, _type_of(grad_out.dtype), n, grad_out.shape[1], gs, kp, kb,
-                                         int(padding_token), float(scale), tp, table_grad.shape[0], ts, wp, wb,
+    rc = lib().gravac_embedding_gradient(gp, _type_of(grad_out.dtype), n, dim, gs, kp, kb, int(padding_token), float(scale), tp, vocab, ts, wp, wb,
                                          FLAG_ACCUMULATE if accumulate else 0, _stream_handle(stream))
     if rc != OK:
         raise GravacError(rc, "gravac_embedding_gradient")
