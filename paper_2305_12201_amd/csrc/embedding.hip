@@ -106,8 +106,8 @@ void launch_lookup(LookupParams& p, int out_type, hipStream_t stream)
 
 constexpr int SORT_T = 1024;                     // threads of a sorting workgroup
 constexpr int SORT_W = SORT_T / 64;
-constexpr int SORT_ROUNDS = 4;                   // tokens per thread in a tile
-constexpr int SORT_TILE = SORT_T * SORT_ROUNDS;  // tokens of a tile
+constexpr int SORT_ROUNDS = 4;                   // tokens per thread in a tile at most
+constexpr int SORT_TILE = SORT_T * SORT_ROUNDS;  // tokens of a tile at most
 constexpr int MAX_BITS = 9;                      // bits of a digit at most: two passes for a vocabulary up to 2^18 - 1
 constexpr int MIN_BITS = 4;
 constexpr int BINS = 1 << MAX_BITS;
@@ -204,14 +204,14 @@ __device__ uint32_t exclusive_sum(uint32_t x, uint32_t* wave_sums)
 // Places of a tile's tokens in the order of one digit, earlier tokens first.  A wavefront's tokens are consecutive, round by
 // round; the lanes of a round that hold the same digit find each other with one ballot per bit.  On return at[r] is the
 // place of the token of round r, and base has moved on by the tile's counts.
-__device__ void place_tile(SortLds& s, int bits, const uint32_t (&digit)[SORT_ROUNDS], const bool (&have)[SORT_ROUNDS],
-                           uint32_t (&at)[SORT_ROUNDS])
+template <int ROUNDS>
+__device__ void place_tile(SortLds& s, int bits, const uint32_t (&digit)[ROUNDS], const bool (&have)[ROUNDS], uint32_t (&at)[ROUNDS])
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, bins = 1 << bits;
     for (int i = threadIdx.x; i < SORT_W * bins; i += SORT_T) s.cnt[i >> bits][i & (bins - 1)] = 0;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < SORT_ROUNDS; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         uint64_t same = __ballot(have[r]);
         for (int b = 0; b < bits; ++b) {
             const bool one = (digit[r] >> b) & 1;
@@ -240,7 +240,7 @@ __device__ void place_tile(SortLds& s, int bits, const uint32_t (&digit)[SORT_RO
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < SORT_ROUNDS; ++r)
+    for (int r = 0; r < ROUNDS; ++r)
         if (have[r]) at[r] += s.cnt[w][digit[r]];
     __syncthreads();
 }
@@ -315,6 +315,7 @@ __global__ __launch_bounds__(SORT_T) void count_kernel(GradParams p, int from, i
 // ... and the tokens moved to their places: behind all smaller digits, and behind the same digit of earlier workgroups.
 // (Workgroups that count all tokens themselves spare a launch per pass and take as long: 16,381 tokens 15.3 us instead of
 // 8.1 and 3 to 5 for the counts.)
+template <int ROUNDS>
 __global__ __launch_bounds__(SORT_T) void scatter_kernel(GradParams p, int from, int to, int shift)
 {
     __shared__ SortLds s;
@@ -342,13 +343,13 @@ __global__ __launch_bounds__(SORT_T) void scatter_kernel(GradParams p, int from,
     const uint32_t first = exclusive_sum(all, s.wave);
     if ((int)threadIdx.x < bins) s.base[threadIdx.x] = first + before;
     __syncthreads();
-    for (int64_t t0 = begin; t0 < end; t0 += SORT_TILE) {
-        uint2 x[SORT_ROUNDS];
-        bool have[SORT_ROUNDS];
-        uint32_t digit[SORT_ROUNDS], at[SORT_ROUNDS];
+    for (int64_t t0 = begin; t0 < end; t0 += SORT_T * ROUNDS) {
+        uint2 x[ROUNDS];
+        bool have[ROUNDS];
+        uint32_t digit[ROUNDS], at[ROUNDS];
 #pragma unroll
-        for (int r = 0; r < SORT_ROUNDS; ++r) {
-            const int64_t i = t0 + (w * SORT_ROUNDS + r) * 64 + lane;
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int64_t i = t0 + (w * ROUNDS + r) * 64 + lane;
             have[r] = i < end;
             x[r] = make_uint2(0, 0);
             if (have[r]) x[r] = from < 0 ? make_uint2(key_at(p, i), (uint32_t)i) : p.pairs[from][i];
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(SORT_T) void scatter_kernel(GradParams p, int from,
         }
         place_tile(s, p.bits, digit, have, at);
 #pragma unroll
-        for (int r = 0; r < SORT_ROUNDS; ++r)
+        for (int r = 0; r < ROUNDS; ++r)
             if (have[r]) p.pairs[to][at[r]] = x[r];
     }
 }
@@ -511,14 +512,14 @@ __global__ __launch_bounds__(64 * SUM_W) void sum_kernel(GradParams p, int sorte
 }
 
 // The runs that cover a share and more: the tail of the share where one begins and the heads of the shares behind it, added up by
-// eight wavefronts, each every eighth share in order, and these sums in order.
-constexpr int JOIN_W = 8;
+// sixteen wavefronts, each every sixteenth share in order, and these sums in order.
+constexpr int JOIN_W = 16;
 constexpr int JOIN_GRID = 1024;
 
 template <bool ADD>
 __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sorted)
 {
-    constexpr int N = 4, U = 4;
+    constexpr int N = 4, U = 8;
     __shared__ float lds[JOIN_W][64][N];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const uint32_t slabs = ((uint32_t)p.dim + 64 * N - 1) / (64 * N);
@@ -732,15 +733,20 @@ void launch_gradient(GradParams& p, const GradLayout& L, hipStream_t stream)
     if (p.n <= SORT_TILE) {
         hipLaunchKernelGGL(sort_few_kernel, dim3(1), dim3(SORT_T), 0, stream, p, passes);
     } else {
-        const int64_t tiles = (p.n + SORT_TILE - 1) / SORT_TILE;
-        p.per_wg = (tiles + SORT_GRID - 1) / SORT_GRID * SORT_TILE;
+        // tiles of one token per thread until a workgroup has several of them: more workgroups, each sooner done (one / four tokens
+        // per thread, us for the call: 5000 of 650 34.4 / 40.6, 16,384 47.7 / 54.5, 131,072 137 / 144; of 256 columns 262,144 118
+        // / 121, 600,000 248 / 253, 1,048,576 412 / 406)
+        const bool one = p.n <= 4 * SORT_GRID * SORT_T;
+        const int64_t tile = one ? SORT_T : SORT_TILE, tiles = (p.n + tile - 1) / tile;
+        p.per_wg = (tiles + SORT_GRID - 1) / SORT_GRID * tile;
         p.sort_wgs = (int32_t)((p.n + p.per_wg - 1) / p.per_wg);
         const dim3 grid((uint32_t)p.sort_wgs);
         int from = -1;
         for (int q = 0; q < passes; ++q) {
             const int to = q & 1;
             hipLaunchKernelGGL(count_kernel, grid, dim3(SORT_T), 0, stream, p, from, q * p.bits);
-            hipLaunchKernelGGL(scatter_kernel, grid, dim3(SORT_T), 0, stream, p, from, to, q * p.bits);
+            if (one) hipLaunchKernelGGL(scatter_kernel<1>, grid, dim3(SORT_T), 0, stream, p, from, to, q * p.bits);
+            else hipLaunchKernelGGL(scatter_kernel<SORT_ROUNDS>, grid, dim3(SORT_T), 0, stream, p, from, to, q * p.bits);
             from = to;
         }
         sorted = from;
