@@ -37,12 +37,24 @@ struct __attribute__((packed, aligned(E::SIZE))) Pack {
 };
 
 template <typename E, int N>
-__device__ __forceinline__ void load(const typename E::word* p, float (&x)[N])
+__device__ __forceinline__ Pack<E, N> fetch(const typename E::word* p)
 {
     Pack<E, N> v;
     __builtin_memcpy(&v, (const Pack<E, N>*)p, sizeof(v));
+    return v;
+}
+
+template <typename E, int N>
+__device__ __forceinline__ void unpack(const Pack<E, N>& v, float (&x)[N])
+{
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = to_float<E>(v.w[i]);
+}
+
+template <typename E, int N>
+__device__ __forceinline__ void load(const typename E::word* p, float (&x)[N])
+{
+    unpack<E, N>(fetch<E, N>(p), x);
 }
 
 template <typename E, int N>
@@ -58,7 +70,8 @@ __device__ __forceinline__ void store(typename E::word* p, const float (&x)[N])
 template <typename E, int N>
 __device__ __forceinline__ void store_streaming(typename E::word* p, const float (&x)[N])
 {
-    constexpr int BYTES = N * E::SIZE, EACH = BYTES < 16 ? BYTES : 16;
+    constexpr int BYTES = N * E::SIZE, EACH = BYTES < 4 ? 4 : BYTES < 16 ? BYTES : 16;
+    if (BYTES < 4) { store<E, N>(p, x); return; }
     typedef uint32_t words __attribute__((ext_vector_type(EACH / 4)));
     typedef words places __attribute__((aligned(E::SIZE)));
     typename E::word w[N];
@@ -88,6 +101,24 @@ __device__ __forceinline__ void store_part(typename E::word* p, int n, const flo
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (i < n) p[i] = from_float<E>(x[i]);
+}
+
+// A lane's N columns of a row of `dim` >= N: the last lane takes the last N, and of those the first `skip` belong to the lane
+// before it.  So every access is a whole one: a load that ends a row by itself is a branch, and a wavefront waits at its end
+// for the loads before it.  skip >= N: nothing is this lane's.
+template <int N>
+struct Columns {
+    int at, skip;
+    __device__ __forceinline__ Columns(int c, int dim) : at(c < dim - N ? c : dim - N), skip(c - at) {}
+};
+
+template <typename E, int N>
+__device__ __forceinline__ void store_behind(typename E::word* p, int skip, const float (&x)[N])
+{
+    if (skip == 0) { store<E, N>(p, x); return; }
+#pragma unroll
+    for (int i = 1; i < N; ++i)
+        if (i >= skip) p[i] = from_float<E>(x[i]);
 }
 
 // Results of more bytes than this are written with the hint that they are not read again soon: half of the 256 MB cache in

@@ -42,11 +42,11 @@ struct LookupParams {
 };
 
 // out[t] = scale * table[tokens[t]]: the product in binary32, then one rounding to the output's type.  A group of `lanes`
-// lanes takes K accesses of a row each, all in flight together; blockIdx.y walks along a row.
-template <typename A, typename B, int K>
+// lanes takes K accesses of a row each, all in flight together; blockIdx.y walks along a row.  A token outside the table reads
+// row 0 and drops it.
+template <typename A, typename B, int N, int K>
 __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p)
 {
-    constexpr int N = 16 / (A::SIZE > B::SIZE ? A::SIZE : B::SIZE);
     const int lane = threadIdx.x & (p.lanes - 1), groups = 256 / p.lanes;
     for (int64_t t = (int64_t)blockIdx.x * groups + threadIdx.x / p.lanes; t < p.n; t += (int64_t)gridDim.x * groups) {
         const int64_t token = token_at(p.tokens, p.wide, t);
@@ -54,24 +54,19 @@ __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p)
         const typename A::word* row = (const typename A::word*)p.table + (inside ? token : 0) * p.table_stride;
         typename B::word* to = (typename B::word*)p.out + t * p.out_stride;
         const int c0 = ((int)blockIdx.y * K * p.lanes + lane) * N;
-        float x[K][N];
+        Pack<A, N> v[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = fetch<A, N>(row + Columns<N>(c0 + k * p.lanes * N, p.dim).at);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = c0 + k * p.lanes * N;
+            const Columns<N> c(c0 + k * p.lanes * N, p.dim);
+            float x[N];
+            unpack<A, N>(v[k], x);
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[k][i] = 0.0f;
-            if (inside && c < p.dim) load_part<A, N>(row + c, p.dim - c, x[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int c = c0 + k * p.lanes * N;
-            if (c >= p.dim) continue;
-            if (inside) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) x[k][i] *= p.scale;
-            }
-            if (p.stream && p.dim - c >= N) store_streaming<B, N>(to + c, x[k]);   // (65,539 rows of 8 KiB: 215 -> 201 us)
-            else store_part<B, N>(to + c, p.dim - c, x[k]);
+            for (int i = 0; i < N; ++i) x[i] = inside ? x[i] * p.scale : 0.0f;
+            if (c.skip >= N) continue;
+            if (p.stream && c.skip == 0) store_streaming<B, N>(to + c.at, x);
+            else store_behind<B, N>(to + c.at, c.skip, x);
         }
     }
 }
@@ -79,8 +74,9 @@ __global__ __launch_bounds__(256) void lookup_kernel(LookupParams p)
 template <typename A, typename B>
 void launch_lookup(LookupParams& p, hipStream_t stream)
 {
-    constexpr int N = 16 / (A::SIZE > B::SIZE ? A::SIZE : B::SIZE);
-    const int64_t chunks = ((int64_t)p.dim + N - 1) / N;
+    constexpr int WIDE = 16 / (A::SIZE > B::SIZE ? A::SIZE : B::SIZE);
+    const bool narrow = p.dim < WIDE;
+    const int64_t n = narrow ? 1 : WIDE, chunks = ((int64_t)p.dim + n - 1) / n;
     p.lanes = 4;
     while (p.lanes < 64 && p.lanes < chunks) p.lanes *= 2;
     const int64_t groups = 256 / p.lanes, rows = (p.n + groups - 1) / groups;
@@ -88,8 +84,9 @@ void launch_lookup(LookupParams& p, hipStream_t stream)
     // four accesses per lane once there are wavefronts enough to fill the card without them
     const int k = p.n * chunks >= (1 << 19) && chunks > p.lanes ? 4 : 1;
     const dim3 grid((uint32_t)x, (uint32_t)((chunks + (int64_t)p.lanes * k - 1) / ((int64_t)p.lanes * k)));
-    if (k == 4) hipLaunchKernelGGL((lookup_kernel<A, B, 4>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((lookup_kernel<A, B, 1>), grid, dim3(256), 0, stream, p);
+    if (narrow) hipLaunchKernelGGL((lookup_kernel<A, B, 1, 1>), grid, dim3(256), 0, stream, p);
+    else if (k == 4) hipLaunchKernelGGL((lookup_kernel<A, B, WIDE, 4>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((lookup_kernel<A, B, WIDE, 1>), grid, dim3(256), 0, stream, p);
 }
 
 template <typename A>
@@ -366,22 +363,23 @@ __global__ __launch_bounds__(SORT_T) void scatter_kernel(GradParams p, int from,
 // gradient: sums
 // ---------------------------------------------------------------------------------------------------------------------
 
-// A row's sum, scaled, into the table: written, or added to what is there (`old`).
+// Columns of a row's sum, scaled, into the table: written, or added to what is there (`old`).
 template <bool ADD, int N>
-__device__ __forceinline__ void put_row(const GradParams& p, uint32_t row, int c, const float (&sum)[N], const float (&old)[N])
+__device__ __forceinline__ void put_row(const GradParams& p, uint32_t row, const Columns<N>& c, const float (&sum)[N], const float (&old)[N])
 {
+    if (c.skip >= N) return;
     float x[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = ADD ? old[i] + p.scale * sum[i] : p.scale * sum[i];
-    uint32_t* to = (uint32_t*)p.table + (int64_t)row * p.table_stride + c;
-    if (!ADD && p.stream && p.dim - c >= N) store_streaming<F32, N>(to, x);
-    else store_part<F32, N>(to, p.dim - c, x);
+    uint32_t* to = (uint32_t*)p.table + (int64_t)row * p.table_stride + c.at;
+    if (!ADD && p.stream && c.skip == 0) store_streaming<F32, N>(to, x);
+    else store_behind<F32, N>(to, c.skip, x);
 }
 
 template <bool ADD, int N>
-__device__ __forceinline__ void get_row(const GradParams& p, uint32_t row, int c, float (&old)[N])
+__device__ __forceinline__ void get_row(const GradParams& p, uint32_t row, const Columns<N>& c, float (&old)[N])
 {
-    if (ADD) load_part<F32, N>((const uint32_t*)p.table + (int64_t)row * p.table_stride + c, p.dim - c, old);
+    if (ADD) load<F32, N>((const uint32_t*)p.table + (int64_t)row * p.table_stride + c.at, old);
 }
 
 // A share of the sorted tokens (1 << share_log of them, at most 64: a lane holds one each) per workgroup, 64 * N columns per
@@ -408,10 +406,10 @@ __device__ __forceinline__ uint32_t first_at_least(const uint2* pairs, uint32_t 
     return lo;
 }
 
-template <typename E, bool ADD>
+template <typename E, bool ADD, int N>
 __global__ __launch_bounds__(64 * SUM_W) void sum_kernel(GradParams p, int sorted)
 {
-    constexpr int N = 16 / E::SIZE, U = 4;
+    constexpr int U = 4;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = (int)blockDim.x >> 6;
     const uint2* pairs = p.pairs[sorted];
     if (blockIdx.x < p.fills) {
@@ -460,10 +458,10 @@ __global__ __launch_bounds__(64 * SUM_W) void sum_kernel(GradParams p, int sorte
         else end = have + follow;
     }
     if (begin == end) return;
-    const int c = (((int)blockIdx.y * waves + w) * 64 + lane) * N;
-    if (c - lane * N >= p.dim) return;
-    const bool active = c < p.dim;
-    const typename E::word* grad = (const typename E::word*)p.grad + c;
+    const int c0 = ((int)blockIdx.y * waves + w) * 64 * N;
+    if (c0 >= p.dim) return;
+    const Columns<N> c(c0 + lane * N, p.dim);
+    const typename E::word* grad = (const typename E::word*)p.grad + c.at;
     if (to_tail && blockIdx.y == 0 && threadIdx.x == 0) p.joins[1 + atomicAdd(&p.joins[0], 1u)] = share;
     row = __builtin_amdgcn_readlane(mine.x, begin < have ? begin : 0);
     float sum[N], kept[N];   // kept: what the table holds in the row of the last token so far
@@ -472,23 +470,25 @@ __global__ __launch_bounds__(64 * SUM_W) void sum_kernel(GradParams p, int sorte
 
     auto flush = [&](bool ends) {
         if (to_head) {
-            if (active) store_part<F32, N>((uint32_t*)p.head + (int64_t)share * p.part_stride + c, p.dim - c, sum);
+            if (c.skip < N) store_behind<F32, N>((uint32_t*)p.head + (int64_t)share * p.part_stride + c.at, c.skip, sum);
             to_head = false;
         } else if (ends && to_tail) {
-            if (active) store_part<F32, N>((uint32_t*)p.tail + (int64_t)share * p.part_stride + c, p.dim - c, sum);
-        } else if (active) {
+            if (c.skip < N) store_behind<F32, N>((uint32_t*)p.tail + (int64_t)share * p.part_stride + c.at, c.skip, sum);
+        } else {
             put_row<ADD, N>(p, row, c, sum, kept);
         }
     };
     auto token_of = [&](int j) { return (uint32_t)(j < have ? __builtin_amdgcn_readlane(mine.x, j) : __builtin_amdgcn_readlane(behind.x, (j - have) & 63)); };
     auto place_of = [&](int j) { return (uint32_t)(j < have ? __builtin_amdgcn_readlane(mine.y, j) : __builtin_amdgcn_readlane(behind.y, (j - have) & 63)); };
     for (int j0 = begin; j0 < end; j0 += U) {
-        float x[U][N], old[U][N];   // old: of the rows whose last token this is, all loads of a round together
+        Pack<E, N> v[U];
+        float old[U][N];   // of the rows whose last token this is; all loads of a round are under way together
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = fetch<E, N>(grad + (int64_t)place_of(j0 + u < end ? j0 + u : end - 1) * p.grad_stride);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u < end ? j0 + u : end - 1;
-            if (active) load_part<E, N>(grad + (int64_t)place_of(j) * p.grad_stride, p.dim - c, x[u]);
-            if (ADD && active && (j + 1 == end || token_of(j + 1) != token_of(j))) get_row<ADD, N>(p, token_of(j), c, old[u]);
+            if (ADD && (j + 1 == end || token_of(j + 1) != token_of(j))) get_row<ADD, N>(p, token_of(j), c, old[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -500,8 +500,10 @@ __global__ __launch_bounds__(64 * SUM_W) void sum_kernel(GradParams p, int sorte
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum[i] = 0.0f;
             }
+            float x[N];
+            unpack<E, N>(v[u], x);
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] += x[u][i];
+            for (int i = 0; i < N; ++i) sum[i] += x[i];
             if (ADD) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) kept[i] = old[u][i];
@@ -521,14 +523,15 @@ __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sor
 {
     constexpr int N = 4, U = 8;
     __shared__ float lds[JOIN_W][64][N];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t slabs = ((uint32_t)p.dim + 64 * N - 1) / (64 * N);
     const uint64_t items = (uint64_t)p.joins[0] * slabs;
     const uint2* pairs = p.pairs[sorted];
     for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const uint32_t share = p.joins[1 + item / slabs];
-        const int c = (int)((uint32_t)(item % slabs) * 64 + lane) * N;
-        const bool active = c < p.dim;
+        // (a part's stride is whole lanes' columns: what lies behind its row is read and dropped)
+        const int c0 = (int)((uint32_t)(item % slabs) * 64 + lane) * N;
+        const Columns<N> c(c0, (int)p.part_stride);
         const uint32_t row = pairs[(((int64_t)share + 1) << p.share_log) - 1].x;
         // the shares behind it that begin with the same token: [share + 1, end), found by looking at 64 of them at a time
         uint32_t lo = share + 1, hi = p.n_shares;   // share `lo` begins with it, share `hi` (if there is one) does not
@@ -546,8 +549,8 @@ __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sor
             float x[U][N];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const uint32_t g = g0 + u * JOIN_W;
-                if (active && g < end) load_part<F32, N>((const uint32_t*)p.head + (int64_t)g * p.part_stride + c, p.dim - c, x[u]);
+                const uint32_t g = g0 + u * JOIN_W < end ? g0 + u * JOIN_W : end - 1;
+                load<F32, N>((const uint32_t*)p.head + (int64_t)g * p.part_stride + c.at, x[u]);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -559,15 +562,18 @@ __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sor
 #pragma unroll
         for (int i = 0; i < N; ++i) lds[w][lane][i] = sum[i];
         __syncthreads();
-        if (w == 0 && active) {
-            load_part<F32, N>((const uint32_t*)p.tail + (int64_t)share * p.part_stride + c, p.dim - c, sum);
+        if (w == 0 && c0 < p.dim) {
+            load<F32, N>((const uint32_t*)p.tail + (int64_t)share * p.part_stride + c.at, sum);
 #pragma unroll
             for (int g = 0; g < JOIN_W; ++g)
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum[i] += lds[g][lane][i];
+            uint32_t* to = (uint32_t*)p.table + (int64_t)row * p.table_stride + c0;
             float old[N];
-            get_row<ADD, N>(p, row, c, old);
-            put_row<ADD, N>(p, row, c, sum, old);
+            if (ADD) load_part<F32, N>(to, p.dim - c0, old);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] = ADD ? old[i] + p.scale * sum[i] : p.scale * sum[i];
+            store_part<F32, N>(to, p.dim - c0, sum);
         }
         __syncthreads();
     }
@@ -581,14 +587,14 @@ __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sor
 // up the rows of all of its kind, its wavefronts in turn, and their sums in order.  The first workgroups clear the rows
 // that no token names.  (700 tokens of 33,278 rows of 650: 16 us, 32 with a sort beside the
 // clearing and two more launches.)
-template <typename E, bool ADD>
+template <typename E, bool ADD, int N>
 __global__ __launch_bounds__(FEW_T) void sum_few_kernel(GradParams p)
 {
-    constexpr int N = 16 / E::SIZE, U = 4;
+    constexpr int U = 4;
     __shared__ uint32_t keys[FEW];
     __shared__ float lds[FEW_W][64][N + 1];
     __shared__ uint32_t named[64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t none = (uint32_t)p.vocab;
     if (blockIdx.x < p.fills) {
         for (uint32_t id = blockIdx.x * gridDim.y + blockIdx.y; id < p.fill_wgs; id += p.fills * gridDim.y) {
@@ -616,25 +622,25 @@ __global__ __launch_bounds__(FEW_T) void sum_few_kernel(GradParams p)
         seen |= __ballot(keys[g * 64 + lane] == row) & before;
     }
     if (seen) return;
-    const int c = ((int)blockIdx.y * 64 + lane) * N;
-    const bool active = c < p.dim;
-    const typename E::word* grad = (const typename E::word*)p.grad + c;
+    const Columns<N> c(((int)blockIdx.y * 64 + lane) * N, p.dim);
+    const typename E::word* grad = (const typename E::word*)p.grad + c.at;
     float sum[N], old[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] = 0.0f;
-    if (w == 0 && active) get_row<ADD, N>(p, row, c, old);
+    if (w == 0) get_row<ADD, N>(p, row, c, old);
     int at = 0, count = 0;   // how many of its kind have been seen, and how many of them wait to be added
-    int wait[U];
+    int wait[U] = {t, t, t, t};
     auto add = [&]() {
-        float x[U][N];
+        Pack<E, N> v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < count && active) load_part<E, N>(grad + (int64_t)wait[u] * p.grad_stride, p.dim - c, x[u]);
+        for (int u = 0; u < U; ++u) v[u] = fetch<E, N>(grad + (int64_t)wait[u] * p.grad_stride);
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u < count) {
+                float x[N];
+                unpack<E, N>(v[u], x);
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[i] += x[u][i];
+                for (int i = 0; i < N; ++i) sum[i] += x[i];
             }
         count = 0;
     };
@@ -648,7 +654,7 @@ __global__ __launch_bounds__(FEW_T) void sum_few_kernel(GradParams p)
             if (++count == U) add();
         }
     }
-    add();
+    if (count > 0) add();
     if (at > 1) {   // the same for all wavefronts
 #pragma unroll
         for (int i = 0; i < N; ++i) lds[w][lane][i] = sum[i];
@@ -659,7 +665,7 @@ __global__ __launch_bounds__(FEW_T) void sum_few_kernel(GradParams p)
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum[i] += lds[v][lane][i];
     }
-    if (w == 0 && active) put_row<ADD, N>(p, row, c, sum, old);
+    if (w == 0) put_row<ADD, N>(p, row, c, sum, old);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -706,10 +712,11 @@ GradLayout grad_layout(int64_t n, int64_t dim)
     return L;
 }
 
-template <typename E, bool ADD>
+// N: columns of a lane (one for rows of less than 16 bytes, so that a row holds a lane's)
+template <typename E, bool ADD, int N>
 void launch_gradient(GradParams& p, const GradLayout& L, hipStream_t stream)
 {
-    const uint32_t slabs = (uint32_t)((p.dim + 64 * (16 / E::SIZE) - 1) / (64 * (16 / E::SIZE)));
+    const uint32_t slabs = (uint32_t)((p.dim + 64 * N - 1) / (64 * N));
     const uint32_t waves = p.n <= FEW ? FEW_W : slabs < SUM_W ? slabs : SUM_W;
     const uint32_t columns = p.n <= FEW ? slabs : (slabs + waves - 1) / waves;   // workgroups side by side
     if (!ADD) {
@@ -721,7 +728,7 @@ void launch_gradient(GradParams& p, const GradLayout& L, hipStream_t stream)
     }
     if (p.n <= FEW) {
         if (p.n + p.fills > 0)
-            hipLaunchKernelGGL((sum_few_kernel<E, ADD>), dim3((uint32_t)p.n + p.fills, slabs), dim3(FEW_T), 0, stream, p);
+            hipLaunchKernelGGL((sum_few_kernel<E, ADD, N>), dim3((uint32_t)p.n + p.fills, slabs), dim3(FEW_T), 0, stream, p);
         return;
     }
     int bits = 1;
@@ -751,15 +758,16 @@ void launch_gradient(GradParams& p, const GradLayout& L, hipStream_t stream)
         }
         sorted = from;
     }
-    hipLaunchKernelGGL((sum_kernel<E, ADD>), dim3(L.n_shares + p.fills, columns), dim3(64 * waves), 0, stream, p, sorted);
+    hipLaunchKernelGGL((sum_kernel<E, ADD, N>), dim3(L.n_shares + p.fills, columns), dim3(64 * waves), 0, stream, p, sorted);
     hipLaunchKernelGGL(join_kernel<ADD>, dim3(JOIN_GRID), dim3(64 * JOIN_W), 0, stream, p, sorted);
 }
 
 template <typename E>
 void launch_gradient(GradParams& p, const GradLayout& L, bool add, hipStream_t stream)
 {
-    if (add) launch_gradient<E, true>(p, L, stream);
-    else launch_gradient<E, false>(p, L, stream);
+    constexpr int WIDE = 16 / E::SIZE;
+    if (p.dim < WIDE) add ? launch_gradient<E, true, 1>(p, L, stream) : launch_gradient<E, false, 1>(p, L, stream);
+    else add ? launch_gradient<E, true, WIDE>(p, L, stream) : launch_gradient<E, false, WIDE>(p, L, stream);
 }
 
 bool misaligned(const void* p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) != 0; }
