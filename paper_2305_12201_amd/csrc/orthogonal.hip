@@ -398,10 +398,11 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
     if (t.mat == NO_MAT) return;
     const Mat d = uniform(p.mats[t.mat]);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int mp = d.mp, width = PRODUCT == GRAM ? d.np : mp;   // length of the sums
+    const int mp = d.mp, width = PRODUCT == GRAM ? d.np : mp;   // elements of an operand's row
     const int64_t left = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : p.flip ? d.xt1 : d.xt0;
     const int64_t right = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : d.q;
-    const int slabs = width / (SPLIT ? 16 : 32);
+    // slabs of a sum, an even number of them (rows hold whole ones: sides are padded to 64 or more); the padding behind is left out
+    const int slabs = (int)padded(PRODUCT == GRAM ? d.n : d.m, SPLIT ? 32 : 64) / (SPLIT ? 16 : 32);
 
     // a wavefront fetches 16 F rows of each operand, sixteen with one instruction: lane l fetches for row l / 4 the chunk
     // whose place is l % 4
@@ -457,7 +458,6 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
     // what stands between two blocks of matrix instructions would leave the matrix core idle (in one block each, it was
     // busy 61 % of the time).
     constexpr int PRODUCTS = SPLIT ? 3 : 2, INSTS = PRODUCTS * F * F, ITEMS = 6 * F;
-    // (sides are padded to 128 elements of two bytes or more: an even number of slabs)
     // A long sum is added up in parts: added one after the other, 70,001 elements of float32 are off by 16 times what the
     // plain evaluation's nested sums are.  (There are no registers for that with tiles of 256, which longer sums do not get.)
     constexpr bool PARTS = F <= 2;
