@@ -420,6 +420,7 @@ int gravac_orthogonalize(const void* in, void* out, int type, int64_t n, const i
  *   params          device, type[n], updated in place (the sum is rounded once to type).
  *   scales          host, float[n_mat], or NULL for 1: the step of each matrix, such as 0.2 sqrt(max(rows, columns)).
  *   flags           0 or GRAVAC_FLAG_NESTEROV.
+ * The three vectors must not overlap.
  */
 int gravac_orthogonal_update(const float* grad, float* momentum, void* params, int type, int64_t n,
                              const int64_t* matrices, int n_mat, float beta, float keep, float alpha, const float* scales,

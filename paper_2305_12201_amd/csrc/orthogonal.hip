@@ -948,6 +948,11 @@ int begin(Call& p, Layout& L, const int64_t* matrices, int n_mat, int type, int6
 
 bool misaligned(const void* p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) != 0; }
 
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
+{
+    return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
+}
+
 }  // namespace
 
 extern "C" {
@@ -969,6 +974,7 @@ int gravac_orthogonalize(const void* in, void* out, int type, int64_t n, const i
     Call p;
     Layout L;
     if (const int rc = begin(p, L, matrices, n_mat, type, n, steps, coefficients, eps, workspace, workspace_bytes)) return rc;
+    if (in != out && overlap(in, n * size_of(type), out, n * size_of(type))) return GRAVAC_ERR_INVALID_ARG;
     p.in = in; p.out = out;
     hipStream_t stream = (hipStream_t)stream_v;
     if (type == GRAVAC_FLOAT32) return run<F32, false, true>(p, L, matrices, nullptr, n_mat, steps, coefficients, stream);
@@ -987,6 +993,9 @@ int gravac_orthogonal_update(const float* grad, float* momentum, void* params, i
     Call p;
     Layout L;
     if (const int rc = begin(p, L, matrices, n_mat, type, n, steps, coefficients, eps, workspace, workspace_bytes)) return rc;
+    if (overlap(grad, 4 * n, momentum, 4 * n) || overlap(grad, 4 * n, params, n * size_of(type)) ||
+        overlap(momentum, 4 * n, params, n * size_of(type)))
+        return GRAVAC_ERR_INVALID_ARG;
     p.grad = grad; p.momentum = momentum; p.out = params;
     p.beta = beta; p.keep = keep; p.alpha = alpha;
     p.nesterov = (flags & GRAVAC_FLAG_NESTEROV) ? 1 : 0;

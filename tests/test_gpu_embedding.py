@@ -197,6 +197,46 @@ def test_gradient_sums_of_whole_numbers_are_exact(dtype, n):
         assert (got[3:].view(vocab, dim + 2)[:, dim:] == 2.0).all() and (got[:3] == 2.0).all()
 
 
+@pytest.mark.parametrize("dim", [1, 2, 3, 4, 5, 7, 8, 9, 11, 255, 257, 259, 511, 513, 519, 2049])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_ends_of_rows(dtype, dim):
+    """Rows that end at any place of a 16-byte access or of a wavefront's columns, strides between them: whole numbers, so that
+    every sum is exact, and what lies between the rows is as it was."""
+    vocab = 23
+    for n in (40, 1500, 4500):
+        g = torch.Generator().manual_seed(dim)
+        whole = torch.randint(-8, 9, (n, dim), generator=g)
+        buf = torch.full((1 + n * (dim + 1),), float("nan"), dtype=dtype)
+        buf[1:].view(n, dim + 1)[:, :dim] = whole.to(dtype)
+        buf = buf.cuda()
+        tokens = _tokens(n, vocab, torch.int32, dim, "padded")
+        ok = (tokens >= 0) & (tokens < vocab)
+        sums = torch.zeros(vocab, dim, dtype=torch.float64).index_add_(0, tokens[ok].long(), whole[ok].double())
+        for accumulate in (False, True):
+            tbuf = torch.full((1 + vocab * (dim + 2),), 3.0, device="cuda")
+            _gradient(buf[1:].view(n, dim + 1)[:, :dim], tokens.cuda(), tbuf[1:].view(vocab, dim + 2)[:, :dim], accumulate=accumulate)
+            got = tbuf.cpu()
+            assert torch.equal(got[1:].view(vocab, dim + 2)[:, :dim].double(), sums + (3.0 if accumulate else 0.0)), (n, accumulate)
+            assert (got[1:].view(vocab, dim + 2)[:, dim:] == 3.0).all() and got[0] == 3.0
+    out = torch.full((1 + 40 * (dim + 2),), 5.0, dtype=dtype, device="cuda")
+    rows = out[1:].view(40, dim + 2)
+    B.gravac_embedding_lookup(buf[1:].view(n, dim + 1)[:vocab, :dim], tokens[:40].cuda(), rows[:, :dim])
+    want = torch.where(ok[:40, None], whole[tokens[:40].long().clamp(0, vocab - 1)], 0)
+    assert torch.equal(rows[:, :dim].cpu().long(), want) and (rows[:, dim:] == 5.0).all() and out[0] == 5.0
+
+
+@pytest.mark.parametrize("n,vocab", [(8192, 700), (8193, 3), (131_073, 9000), (200_003, 4000), (524_288, 70), (524_289, 1 << 19)])
+def test_gradient_of_many_tokens_is_exact(n, vocab):
+    """Whole numbers up to 8 in magnitude: sums of at most 2^20 of them are exact."""
+    dim = 12
+    g = torch.Generator().manual_seed(n)
+    whole = torch.randint(-8, 9, (n, dim), generator=g)
+    tokens = _tokens(n, vocab, torch.int64, 3, "text")
+    table = torch.full((vocab, dim), float("nan"), device="cuda")
+    _gradient(whole.to(torch.bfloat16).cuda(), tokens.cuda(), table)
+    assert torch.equal(table.cpu().double(), torch.zeros(vocab, dim, dtype=torch.float64).index_add_(0, tokens, whole.double()))
+
+
 def test_gradient_of_no_tokens():
     table = torch.ones(10, 6, device="cuda")
     none, tokens = torch.empty(0, 6, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda")

@@ -69,6 +69,15 @@ def test_update_refuses(bad):
     assert _update(**bad) == B.ERR_INVALID_ARG
 
 
+def test_refuses_vectors_that_overlap():
+    # 1000 elements: 4000 bytes, or 2000 of bfloat16
+    assert _orthogonalize(x=0x1000, out=0x1000 + 3996) == B.ERR_INVALID_ARG
+    assert _orthogonalize(x=0x1000 + 1998, out=0x1000, type=B.BFLOAT16) == B.ERR_INVALID_ARG
+    for bad in ({"grad": 0x2000}, {"momentum": 0x3000}, {"params": 0x1000}, {"grad": 0x2000 - 3996}, {"params": 0x2000 - 1998, "type": B.FLOAT16},
+                {"params": 0x1000 + 3996, "type": B.BFLOAT16}):
+        assert _update(**bad) == B.ERR_INVALID_ARG
+
+
 @pytest.mark.parametrize("triple", [(float("nan"), 0, 0), (1, float("inf"), 0), (4.0, 0, 0), (1.0, 3.0, 0), (0, 0, 3.95), (1.0, -16.0, 0),
                                     (0, 0, 1e9)])
 def test_refuses_coefficients_that_leave_the_range(triple):
