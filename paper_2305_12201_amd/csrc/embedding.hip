@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "elements.h"
 #include "gravac.h"
@@ -514,8 +515,9 @@ __global__ __launch_bounds__(64 * SUM_W) void sum_kernel(GradParams p, int sorte
 }
 
 // The runs that cover a share and more: the tail of the share where one begins and the heads of the shares behind it, added up by
-// sixteen wavefronts, each every sixteenth share in order, and these sums in order.
-constexpr int JOIN_W = 16;
+// eight wavefronts, each every eighth share in order, and these sums in order.  Eight loads are under way together, but two at the end:
+// most runs are short (131,072 tokens of 4096: 24 us, 33 with eights alone; one of 440,000 tokens: 233 us, 283 with fours alone).
+constexpr int JOIN_W = 8;
 constexpr int JOIN_GRID = 1024;
 
 template <bool ADD>
@@ -545,20 +547,23 @@ __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sor
         }
         const uint32_t end = lo + 1;
         float sum[N] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (uint32_t g0 = share + 1 + w; g0 < end; g0 += JOIN_W * U) {
-            float x[U][N];
+        uint32_t g = share + 1 + w;
+        auto add = [&](auto count) {   // of this wavefront's next shares, loads together (behind the last one: of it again)
+            constexpr int M = decltype(count)::value;
+            float x[M][N];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t g = g0 + u * JOIN_W < end ? g0 + u * JOIN_W : end - 1;
-                load<F32, N>((const uint32_t*)p.head + (int64_t)g * p.part_stride + c.at, x[u]);
-            }
+            for (int u = 0; u < M; ++u)
+                load<F32, N>((const uint32_t*)p.head + (int64_t)(g + u * JOIN_W < end ? g + u * JOIN_W : end - 1) * p.part_stride + c.at, x[u]);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (g0 + u * JOIN_W < end) {
+            for (int u = 0; u < M; ++u)
+                if (g + u * JOIN_W < end) {
 #pragma unroll
                     for (int i = 0; i < N; ++i) sum[i] += x[u][i];
                 }
-        }
+            g += M * JOIN_W;
+        };
+        while (g + (U - 1) * JOIN_W < end) add(std::integral_constant<int, U>());
+        while (g < end) add(std::integral_constant<int, 2>());
 #pragma unroll
         for (int i = 0; i < N; ++i) lds[w][lane][i] = sum[i];
         __syncthreads();
