@@ -9,15 +9,21 @@
 // Numbers.  Operands are binary16, sums binary32.  A matrix of float32 or float16 (or of parameters of that type) is cut into
 // two binary16 parts, x = hi + lo, 22 bits, and a product is hi hi + hi lo + lo hi: as exact as products in binary32 (the
 // dropped lo lo is 2^-22 of the product), at three matrix instructions in place of the sixteen times slower binary32 ones.
-// For bfloat16 the products take hi alone, 11 bits, which costs less than the result's rounding to 8 bits.  Three things keep their rounding (2^-12 relative) from growing
-// with the steps, which multiply a small singular value by a each: the term a X is taken in binary32 from hi + lo;
+// For bfloat16 the products take hi alone, 11 bits, which costs less than the result's rounding to 8 bits.  Three things keep
+// their rounding (2^-12 relative) from growing with the steps, which multiply a small singular value by a each: the term a X is
+// taken in binary32 from hi + lo;
 // the diagonals of A and P, far larger than the rest, are kept in binary32 outside the products,
 //     A = D + E:  A A = E E + (d_i + d_j) e_ij + [i = j] d_i^2,      P = D' + Q:  X <- (a + d'_i) x_i + Q X;
 // and every operand is scaled by a power of two so that typical entries lie near 1 and the largest one possible below 65504.
 //
 // Memory.  Every product is of the form C = L R^T with rows of L and R contiguous along the sum: X is kept as X and as X^T,
 // both written by the product that makes them.  Rows and columns are padded with zeros to whole tiles, so the products have
-// no edges.
+// no edges; their sums end with the matrix (four 2600 x 650 in float32: 511 -> 473 us).
+//
+// Measured, five steps: 4096 x 4096 in bfloat16 1.48 to 1.63 ms (845 to 930 TFLOP/s of what is not symmetric; the clock gives way to
+// power there: 1.7 GHz), the 16 matrices of the VGG16 shape in float32 21.8 to 22.4 ms (three products each: 1130 TFLOP/s of matrix
+// instructions), the 105 of ResNet101 1.83 to 1.87 ms, where X, of 178 MB, passes memory four times a step, 512 x 128 in bfloat16 76 us,
+// 15 products one after the other at 3 to 4 us.
 
 #include <hip/hip_runtime.h>
 
@@ -383,8 +389,8 @@ __device__ __forceinline__ float take_diagonal(float (&v)[8], bool on_diagonal, 
     return x;
 }
 
-// C = L R^T on tiles of 64 F x 64 F (F = 1, 2, 4), four wavefronts of 32 F x 32 F.  A slab of an operand is 64 F rows of SLAB bytes in LDS;
-// the 16-byte chunks of a row are stored in an order turned by the row, so that the lanes that read one chunk of eight
+// C = L R^T on tiles of 64 F x 64 F (F = 1, 2, 4), four wavefronts of 32 F x 32 F.  A slab of an operand is 64 F rows of SLAB
+// bytes in LDS; the 16-byte chunks of a row are stored in an order turned by the row, so that the lanes that read one chunk of eight
 // consecutive rows touch all banks.  While a slab is multiplied from registers, the next is read from LDS into others and
 // those behind it are on their way from memory, BUFFERS - 2 of them.
 template <Product PRODUCT, bool SPLIT, typename E, bool UPDATE, int F, int BUFFERS>
@@ -507,7 +513,7 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
     // the rest of the arithmetic with 16-byte accesses; what it writes along the right index goes through LDS once more.
     // Column j of the block holds its 16 groups of four rows in an order turned by j + 2 (j / 8): four rows of a column as
     // the matrix instructions leave them, eight rows of a column and eight columns of a row all touch the banks evenly.
-    // (Four bytes at a time in rows of 65: 3.4 us of a kernel's 5.8, now PLACE.)
+    // (Four bytes at a time in rows of 65 the epilogue of X took 3.4 us for a 128 x 512 matrix in bfloat16, so 2.7.)
     float* block = (float*)lds + w * SIDE * SIDE;
     auto spot = [](int i, int j) { return j * SIDE + (((i >> 2) + j + 2 * (j >> 3)) & (SIDE / 4 - 1)) * 4 + (i & 3); };
     constexpr int BLOCKS = 32 * F / SIDE, EIGHTS = SIDE / 8, COLUMNS = 64 / EIGHTS;   // lanes: eights of a column, columns
@@ -687,7 +693,7 @@ int64_t large_side(const int64_t* matrix) { return std::max(matrix[1], matrix[2]
 
 // Side of the products' tiles.  Tiles of 256 need half the LDS traffic, but there are a quarter as many and more of them is
 // padding: they pay where A has tiles for half of the compute units, from matrices of four or more a side that are most of the
-// work.  Measured in us with tiles of 128 and of 256, five steps in float32 / bfloat16: 2560 x 5120 1857 and 2831 /
+// work.  Measured in us with tiles of 128 and of 256, five steps in float32 / bfloat16, sums over the padding too: 2560 x 5120 1857 and 2831 /
 // 832 and 1183 (55 tiles of A), twelve 1024 x 1024 999 and 1214 / 579 and 615 (120), four 2048 x 2048 2269 and 2318 /
 // 1027 and 1011 (144), 4096 x 4096 4119 and 4064 / 1738 and 1636 (136), twelve 1500 x 3000 4881 and 4722 / 2395 and 2213 (252).
 int tile_of(const int64_t* matrices, int n_mat)
@@ -713,7 +719,7 @@ uint64_t tiles_of(const int64_t* matrix, int k, int64_t side, int64_t pad)
 }
 
 // Tiles of 64 where those of 128 would be few: they bring more compute units to work and their epilogues are short.  us for five
-// steps in float32, with A, P and X in tiles of 128 / A in 64 / A and P / all: 512 x 512 234, 202, 165, 135; 1024 x 1024 344,
+// steps in float32, sums over the padding too, with A, P and X in tiles of 128 / A in 64 / A and P / all: 512 x 512 234, 202, 165, 135; 1024 x 1024 344,
 // 297, 241, 197; four 2600 x 650 (84 tiles of 128 of A and P, 504 of X) 548, 492, 465, 542; 1536 x 1536 (78, 144) 464, 438, 398,
 // 418; four 1024 x 1024 (144, 256) 427, 439, 438, 469; the ResNet101 shape (405, 2700) with P alone in 64 1924 -> 1863.
 // Twelve 300 x 900 are 245 with X in 128 and 228 in 64 for the padding alone.
