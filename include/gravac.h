@@ -378,9 +378,7 @@ int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tok
  *                   everything else of the flat vectors (biases, embeddings) is neither read nor written.
  *   n               elements of the flat vectors, 1 .. 2^40.
  *   type            GRAVAC_FLOAT32, GRAVAC_BFLOAT16 or GRAVAC_FLOAT16: elements of in and out, or of the parameters.  The
- *                   products are as exact as in binary32, except with GRAVAC_BFLOAT16: there their operands are rounded to
- *                   11 bits, which loses less than the result's own rounding to 8 (singular values of one matrix that are
- *                   thousands of times apart can lose more: a step multiplies the smallest by a, their rounding with them).
+ *                   products are as exact as in binary32 with all of them; a 16-bit result is rounded once, at the end.
  *   steps           1 .. GRAVAC_MAX_STEPS.
  *   coefficients    host, double[steps][3]: a, b, c of each step; NULL for 3.4445, -4.7750, 2.0315 in all of them.  Refused
  *                   where a step could take a singular value above 3.9, or |b s^2 + c s^4| above 15: from singular values in
@@ -388,8 +386,8 @@ int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tok
  *   eps             >= 0 and finite.  A matrix of zeros gives zeros, also with eps = 0; one with a NaN or an infinity gives
  *                   NaN in all of its elements and changes no other matrix.
  *   workspace       device, 256-byte aligned, at least gravac_orthogonalize_workspace_bytes(matrices, n_mat, type) bytes:
- *                   about 12 per element of the matrices (8 with GRAVAC_BFLOAT16), sides rounded up to whole tiles,
- *                   and 8 (4) per element of a square of the smaller side.
+ *                   about 12 per element of the matrices, sides rounded up to whole tiles, and 8 per element of a square of
+ *                   the smaller side.
  *
  * The calls consist of kernel launches only and can be recorded into a graph; the host tables are read at capture time.
  */

@@ -6,12 +6,12 @@
 // which maps every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors.  All three products are of
 // matrix-core kind and bound the call; A and P are symmetric, so half of their tiles are computed and written twice.
 //
-// Numbers.  Operands are binary16, sums binary32.  A matrix of float32 or float16 (or of parameters of that type) is cut into
-// two binary16 parts, x = hi + lo, 22 bits, and a product is hi hi + hi lo + lo hi: as exact as products in binary32 (the
-// dropped lo lo is 2^-22 of the product), at three matrix instructions in place of the sixteen times slower binary32 ones.
-// For bfloat16 the products take hi alone, 11 bits, which costs less than the result's rounding to 8 bits.  Three things keep
-// their rounding (2^-12 relative) from growing with the steps, which multiply a small singular value by a each: the term a X is
-// taken in binary32 from hi + lo;
+// Numbers.  Operands are binary16, sums binary32.  A matrix is cut into two binary16 parts, x = hi + lo, 22 bits, and a product
+// is hi hi + hi lo + lo hi: as exact as products in binary32 (the dropped lo lo is 2^-22 of the product), at three matrix
+// instructions in place of the sixteen times slower binary32 ones.  That holds for 16-bit matrices and parameters too, whose
+// steps are as exact: with hi alone, 11 bits, a bfloat16 result is off by 6e-4 before its own rounding and one entry in
+// five is not the nearest one, for a third of the matrix instructions.  Three things keep the operands' rounding from growing
+// with the steps, which multiply a small singular value by a each: the term a X is taken in binary32 from hi + lo;
 // the diagonals of A and P, far larger than the rest, are kept in binary32 outside the products,
 //     A = D + E:  A A = E E + (d_i + d_j) e_ij + [i = j] d_i^2,      P = D' + Q:  X <- (a + d'_i) x_i + Q X;
 // and every operand is scaled by a power of two so that typical entries lie near 1 and the largest one possible below 65504.
@@ -20,10 +20,10 @@
 // both written by the product that makes them.  Rows and columns are padded with zeros to whole tiles, so the products have
 // no edges; their sums end with the matrix (four 2600 x 650 in float32: 511 -> 473 us).
 //
-// Measured, five steps: 4096 x 4096 in bfloat16 1.48 to 1.63 ms (845 to 930 TFLOP/s of what is not symmetric; the clock gives way to
-// power there: 1.7 GHz), the 16 matrices of the VGG16 shape in float32 21.8 to 22.4 ms (three products each: 1130 TFLOP/s of matrix
-// instructions), the 105 of ResNet101 1.83 to 1.87 ms, where X, of 178 MB, passes memory four times a step, 512 x 128 in bfloat16 76 us,
-// 15 products one after the other at 3 to 4 us.
+// Measured, five steps: 4096 x 4096 in bfloat16 3.82 ms (three products each: 1080 TFLOP/s of matrix instructions; the clock gives way
+// to power there: 1.7 GHz), the 16 matrices of the VGG16 shape in float32 21.8 to 22.4 ms (1130 TFLOP/s), the 105 of ResNet101 1.83
+// to 1.87 ms, where X, of 178 MB, passes memory four times a step, 512 x 128 in bfloat16 93 us, 15 products one after the other at 4 to
+// 6 us.
 
 #include <hip/hip_runtime.h>
 
@@ -43,13 +43,13 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-constexpr int SLAB = 64;           // bytes of an operand's row that are fetched at a time: 16 elements as hi and lo, or 32 hi
+constexpr int SLAB = 64;           // bytes of an operand's row that are fetched at a time: 16 elements as hi and lo
 constexpr int PART_SLABS = 128;    // slabs of a sum that are added one after the other (tiles of 128)
 constexpr int64_t LONG_SIDE = 32768;   // no tiles of 256 for longer sums
 constexpr int BLOCK = 128;         // rows whose slabs stand together in memory
 constexpr int MAX_MAT = GRAVAC_MAX_MATRICES;
 constexpr int MAX_PARTS = 1024;    // partial sums of a matrix's norm at most
-constexpr int PART = 4096;         // elements of one, at least
+constexpr int PART = 16384;        // bytes of one in the matrix's type, at least
 constexpr int PER_INIT = 48;       // matrices of one launch of the table kernel (its argument holds them)
 constexpr int CUT = 64;            // side of a tile of the kernel that cuts a matrix into operands
 
@@ -70,7 +70,7 @@ struct Mat {     // ... and what the kernels read
     uint32_t cut, part, parts;
     float scale;
     float sx, sa, sq;                 // powers of two: X, E and Q are stored multiplied by them
-    int64_t x, xt0, xt1, lo, e, q, da, dq;   // byte offsets in the workspace
+    int64_t x, xt0, xt1, e, q, da, dq;   // byte offsets in the workspace
 };
 
 struct Tile { uint32_t mat; uint16_t i, j; };
@@ -94,20 +94,19 @@ __host__ __device__ inline float power_of_two(double x, int most)
 }
 
 // Lays out a matrix's part of the workspace; returns its size.
-__host__ __device__ inline int64_t lay_out(Mat& d, int64_t rows, int64_t cols, int64_t base, bool split, int tile)
+__host__ __device__ inline int64_t lay_out(Mat& d, int64_t rows, int64_t cols, int64_t base, int tile)
 {
     d.rows = (int32_t)rows; d.cols = (int32_t)cols;
     d.tall = rows > cols;
     d.m = (int32_t)(d.tall ? cols : rows); d.n = (int32_t)(d.tall ? rows : cols);
     d.mp = (int32_t)padded(d.m, tile); d.np = (int32_t)padded(d.n, tile);
     // (the rows of an operand stand in blocks)
-    const int64_t el = split ? 4 : 2, mb = padded(d.mp, BLOCK), nb = padded(d.np, BLOCK);
+    const int64_t el = 4, mb = padded(d.mp, BLOCK), nb = padded(d.np, BLOCK);
     const int64_t xb = aligned(el * mb * d.np), tb = aligned(el * nb * d.mp), ab = aligned(el * mb * d.mp);
     int64_t at = base;
     d.x = at; at += xb;
     d.xt0 = at; at += tb;
     d.xt1 = at; at += tb;
-    d.lo = at; at += split ? 0 : xb;
     d.e = at; at += ab;
     d.q = at; at += ab;
     d.da = at; at += aligned(4 * (int64_t)d.mp);
@@ -142,7 +141,7 @@ struct Call {
 // ---------------------------------------------------------------------------------------------------------------------
 
 struct InitArgs {
-    int32_t n, first, split, tile, side[3];
+    int32_t n, first, tile, side[3];
     Stretches list[3];
     MatIn mat[PER_INIT];
 };
@@ -178,7 +177,7 @@ __global__ __launch_bounds__(256) void table_kernel(Call p, InitArgs a)
     const MatIn& g = a.mat[blockIdx.x];
     const uint32_t id = (uint32_t)(a.first + blockIdx.x);
     Mat d;
-    lay_out(d, g.rows, g.cols, g.base, a.split != 0, a.tile);
+    lay_out(d, g.rows, g.cols, g.base, a.tile);
     d.offset = g.offset; d.stride = g.stride;
     d.cut = g.cut; d.part = g.part; d.parts = g.parts; d.scale = g.scale;
     if (threadIdx.x == 0) p.mats[id] = d;
@@ -274,17 +273,14 @@ __device__ __forceinline__ void cut_in_two(float x, _Float16& hi, _Float16& lo)
 }
 
 // Where element k of a row of an operand lies, in binary16 elements: the slabs of 128 rows stand one behind the other, so
-// what a product fetches at a time is contiguous.  In two parts, a row of a slab is 16 hi and their 16 lo.  `width`: elements
-// of a row.
-template <bool SPLIT>
+// what a product fetches at a time is contiguous.  A row of a slab is 16 hi and their 16 lo.  `width`: elements of a row.
 __device__ __forceinline__ int64_t place(int row, int width, int k)
 {
-    constexpr int EACH = SPLIT ? 16 : 32, LOG = SPLIT ? 4 : 5;
-    return ((int64_t)(row >> 7) * (width >> LOG) + (k >> LOG)) * (BLOCK * 32) + (row & (BLOCK - 1)) * 32 + (k & (EACH - 1));
+    return ((int64_t)(row >> 7) * (width >> 4) + (k >> 4)) * (BLOCK * 32) + (row & (BLOCK - 1)) * 32 + (k & 15);
 }
 
 // X and X^T as operands, from the matrix over its norm; zeros in the padding.
-template <typename E, bool UPDATE, bool SPLIT>
+template <typename E, bool UPDATE>
 __global__ __launch_bounds__(256) void cut_kernel(Call p)
 {
     __shared__ double lds[4];
@@ -310,7 +306,7 @@ __global__ __launch_bounds__(256) void cut_kernel(Call p)
         for (int q = 0; q < 4; ++q) buf[r][c + q] = (float)((double)x[q] * inv);
     }
     __syncthreads();
-    _Float16 *x = (_Float16*)(p.ws + d.x), *xt = (_Float16*)(p.ws + d.xt0), *lo = (_Float16*)(p.ws + d.lo);
+    _Float16 *x = (_Float16*)(p.ws + d.x), *xt = (_Float16*)(p.ws + d.xt0);
     for (int e = threadIdx.x; e < 2 * CUT * CUT / 8; e += 256) {
         const bool second = e >= CUT * CUT / 8;                    // X^T
         const int row = (e & (CUT * CUT / 8 - 1)) / (CUT / 8), k = (e % (CUT / 8)) * 8;
@@ -323,10 +319,9 @@ __global__ __launch_bounds__(256) void cut_kernel(Call p)
             cut_in_two(v, hi, low);
             h[q] = hi; l[q] = low;
         }
-        const int64_t at = second ? place<SPLIT>(j0 + row, d.mp, i0 + k) : place<SPLIT>(i0 + row, d.np, j0 + k);
+        const int64_t at = second ? place(j0 + row, d.mp, i0 + k) : place(i0 + row, d.np, j0 + k);
         *(half8*)((second ? xt : x) + at) = h;
-        if (SPLIT) *(half8*)((second ? xt : x) + at + LOW) = l;
-        else if (!second) *(half8*)(lo + at) = l;
+        *(half8*)((second ? xt : x) + at + LOW) = l;
     }
 }
 
@@ -393,7 +388,7 @@ __device__ __forceinline__ float take_diagonal(float (&v)[8], bool on_diagonal, 
 // bytes in LDS; the 16-byte chunks of a row are stored in an order turned by the row, so that the lanes that read one chunk of eight
 // consecutive rows touch all banks.  While a slab is multiplied from registers, the next is read from LDS into others and
 // those behind it are on their way from memory, BUFFERS - 2 of them.
-template <Product PRODUCT, bool SPLIT, typename E, bool UPDATE, int F, int BUFFERS>
+template <Product PRODUCT, typename E, bool UPDATE, int F, int BUFFERS>
 __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) void product_kernel(Call p)
 {
     constexpr int T = 64 * F, LOADS = 2 * F;              // a wavefront's loads per slab
@@ -408,14 +403,14 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
     const int64_t left = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : p.flip ? d.xt1 : d.xt0;
     const int64_t right = PRODUCT == GRAM ? d.x : PRODUCT == POLY ? d.e : d.q;
     // slabs of a sum, an even number of them (rows hold whole ones: sides are padded to 64 or more); the padding behind is left out
-    const int slabs = (int)padded(PRODUCT == GRAM ? d.n : d.m, SPLIT ? 32 : 64) / (SPLIT ? 16 : 32);
+    const int slabs = (int)padded(PRODUCT == GRAM ? d.n : d.m, 32) / 16;
 
     // a wavefront fetches 16 F rows of each operand, sixteen with one instruction: lane l fetches for row l / 4 the chunk
     // whose place is l % 4
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     const uint32_t fetch_at = (uint32_t)((lane >> 2) * SLAB + ((lane & 3) ^ ((lane >> 4) & 3)) * 16);
-    const char* from_left = uniform(p.ws + left + 2 * place<SPLIT>(t.i * T + w * 16 * F, width, 0));
-    const char* from_right = uniform(p.ws + right + 2 * place<SPLIT>(t.j * T + w * 16 * F, width, 0));
+    const char* from_left = uniform(p.ws + left + 2 * place(t.i * T + w * 16 * F, width, 0));
+    const char* from_right = uniform(p.ws + right + 2 * place(t.j * T + w * 16 * F, width, 0));
     const uint32_t fetch_to = lds0 + (uint32_t)(w * 16 * F) * SLAB;
     // load number `q` of a slab's 2 F (behind the last slab: of that one again, so that as many are always under way)
     auto fetch = [&](int slab, int q) {
@@ -433,14 +428,14 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
     };
     const int wi = (w >> 1) * 32 * F, wj = (w & 1) * 32 * F;
     const int frag_row = lane & 31, frag_half = lane >> 5;
-    // a slab's fragments: two each of 32 rows by 16 elements (SPLIT: hi and lo of the same)
+    // a slab's fragments: hi and lo of 32 rows by 16 elements each
     half8 l[2][2][F], r[2][2][F];
     const int chunk0 = (frag_half ^ ((frag_row >> 2) & 3)) * 16, chunk1 = chunk0 ^ 32;
     // fragment number `q` of a slab's 4 F, in the order of their use
     auto read = [&](int slab, int set, int q) {
         const char* at = lds + (slab & (BUFFERS - 1)) * 2 * T * SLAB + frag_row * SLAB;
         const int h = q / (2 * F), i = q % F, o = q / F % 2;
-        const int part = SPLIT && o ? 1 - h : h;      // the first product takes hi of the left and lo of the right
+        const int part = o ? 1 - h : h;      // the first product takes hi of the left and lo of the right
         const char* from = at + (part ? chunk1 : chunk0) + (o ? T + wj + i * 32 : wi + i * 32) * SLAB;
         if (o) r[set][part][i] = *(const half8*)from;
         else l[set][part][i] = *(const half8*)from;
@@ -463,7 +458,7 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
     // The matrix instructions of a slab, with what brings in the others between them: a wavefront is alone on its SIMD, so
     // what stands between two blocks of matrix instructions would leave the matrix core idle (in one block each, it was
     // busy 61 % of the time).
-    constexpr int PRODUCTS = SPLIT ? 3 : 2, INSTS = PRODUCTS * F * F, ITEMS = 6 * F;
+    constexpr int PRODUCTS = 3, INSTS = PRODUCTS * F * F, ITEMS = 6 * F;
     // A long sum is added up in parts: added one after the other, 70,001 elements of float32 are off by 16 times what the
     // plain evaluation's nested sums are.  (There are no registers for that with tiles of 256, which longer sums do not get.)
     constexpr bool PARTS = F <= 2;
@@ -494,7 +489,7 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
                     else read(s + 1, 1 - u, q - q / 3 - 1);
                 }
                 const int k = m / (F * F), i = m / F % F, j = m % F;
-                const int a = SPLIT ? (k == 1 ? 1 : 0) : k, b = SPLIT ? (k == 0 ? 1 : 0) : k;
+                const int a = k == 1 ? 1 : 0, b = k == 0 ? 1 : 0;
                 acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[u][a][i], r[u][b][j], acc[i][j], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -513,7 +508,7 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
     // the rest of the arithmetic with 16-byte accesses; what it writes along the right index goes through LDS once more.
     // Column j of the block holds its 16 groups of four rows in an order turned by j + 2 (j / 8): four rows of a column as
     // the matrix instructions leave them, eight rows of a column and eight columns of a row all touch the banks evenly.
-    // (Four bytes at a time in rows of 65 the epilogue of X took 3.4 us for a 128 x 512 matrix in bfloat16, so 2.7.)
+    // (Four bytes at a time in rows of 65 the epilogue of X took 3.4 us for a 128 x 512 matrix of operands in one part, so 2.7.)
     float* block = (float*)lds + w * SIDE * SIDE;
     auto spot = [](int i, int j) { return j * SIDE + (((i >> 2) + j + 2 * (j >> 3)) & (SIDE / 4 - 1)) * 4 + (i & 3); };
     constexpr int BLOCKS = 32 * F / SIDE, EIGHTS = SIDE / 8, COLUMNS = 64 / EIGHTS;   // lanes: eights of a column, columns
@@ -540,10 +535,10 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
 #pragma unroll
                 for (int it = 0; it < ROWS; ++it) {
                     const int j = j0 + it * COLUMNS + column;
-                    const int64_t at = place<SPLIT>(j, mp, i);
+                    const int64_t at = place(j, mp, i);
                     mj[it] = da[j];
                     mh[it] = *(const half8*)(e + at);
-                    if (SPLIT) ml[it] = *(const half8*)(e + at + LOW);
+                    ml[it] = *(const half8*)(e + at + LOW);
                 }
             } else if (PRODUCT == NEXT || PRODUCT == LAST) {
                 // i: along n, j: along m
@@ -552,10 +547,10 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
 #pragma unroll
                 for (int it = 0; it < ROWS; ++it) {
                     const int j = j0 + it * COLUMNS + column;
-                    const int64_t at = place<SPLIT>(j, d.np, i);
+                    const int64_t at = place(j, d.np, i);
                     mj[it] = p.a + dq[j];
                     mh[it] = *(const half8*)(x + at);
-                    ml[it] = SPLIT ? *(const half8*)(x + at + LOW) : *(const half8*)((const _Float16*)(ws + d.lo) + at);
+                    ml[it] = *(const half8*)(x + at + LOW);
                 }
             }
             // acc[4 g + q] of lane l is row 8 g + 4 (l / 32) + q, column l % 32 of its 32 x 32
@@ -596,7 +591,7 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
                     const float dj = mj[it], sa = 1.0f / d.sa;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
-                        const float eij = ((float)mh[it][q] + (SPLIT ? (float)ml[it][q] : 0.0f)) * sa;
+                        const float eij = ((float)mh[it][q] + (float)ml[it][q]) * sa;
                         v[q] = (p.b * eij + p.c * (v[q] * (sa * sa) + (mi[q] + dj) * eij)) * d.sq;
                     }
                     const float pjj = take_diagonal(v, i0 == j0, j - i);   // (e_jj = 0: c times the sum)
@@ -608,11 +603,10 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
                 }
                 if (PRODUCT != LAST) {
                     cut_8(v, h, l);
-                    const int64_t at = place<SPLIT>(j, PRODUCT == NEXT ? d.np : mp, i);
+                    const int64_t at = place(j, PRODUCT == NEXT ? d.np : mp, i);
                     _Float16* to = (_Float16*)(ws + (PRODUCT == GRAM ? d.e : PRODUCT == POLY ? d.q : d.x));
                     *(half8*)(to + at) = h;
-                    if (SPLIT) *(half8*)(to + at + LOW) = l;
-                    else if (PRODUCT == NEXT) *(half8*)((_Float16*)(ws + d.lo) + at) = l;
+                    *(half8*)(to + at + LOW) = l;
                 } else {
                     const float sx = 1.0f / d.sx, step = p.alpha * d.scale;
 #pragma unroll
@@ -655,10 +649,10 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
                     } else {
                         half8 h, l;
                         cut_8(v, h, l);
-                        const int64_t at = place<SPLIT>(i, mp, j);
+                        const int64_t at = place(i, mp, j);
                         _Float16* to = (_Float16*)(ws + (PRODUCT == GRAM ? d.e : PRODUCT == POLY ? d.q : p.flip ? d.xt0 : d.xt1));
                         *(half8*)(to + at) = h;
-                        if (SPLIT) *(half8*)(to + at + LOW) = l;
+                        *(half8*)(to + at + LOW) = l;
                     }
                 }
             }
@@ -682,9 +676,9 @@ struct Layout {
     int64_t mats, tile_at[3], part_sums, cut_of, part_of, data, total;
 };
 
-int parts_of(int64_t rows, int64_t cols)
+int parts_of(int64_t rows, int64_t cols, int type)
 {
-    const int64_t n = (rows * cols + PART - 1) / PART;
+    const int64_t n = (rows * cols * size_of(type) + PART - 1) / PART;
     return (int)(n < MAX_PARTS ? n : MAX_PARTS);
 }
 
@@ -693,9 +687,9 @@ int64_t large_side(const int64_t* matrix) { return std::max(matrix[1], matrix[2]
 
 // Side of the products' tiles.  Tiles of 256 need half the LDS traffic, but there are a quarter as many and more of them is
 // padding: they pay where A has tiles for half of the compute units, from matrices of four or more a side that are most of the
-// work.  Measured in us with tiles of 128 and of 256, five steps in float32 / bfloat16, sums over the padding too: 2560 x 5120 1857 and 2831 /
-// 832 and 1183 (55 tiles of A), twelve 1024 x 1024 999 and 1214 / 579 and 615 (120), four 2048 x 2048 2269 and 2318 /
-// 1027 and 1011 (144), 4096 x 4096 4119 and 4064 / 1738 and 1636 (136), twelve 1500 x 3000 4881 and 4722 / 2395 and 2213 (252).
+// work.  Measured in us with tiles of 128 and of 256, five steps, sums over the padding too: 2560 x 5120 1857 and 2831 (55 tiles of A), twelve
+// 1024 x 1024 999 and 1214 (120), four 2048 x 2048 2269 and 2318 (144), 4096 x 4096 4119 and 4064 (136), twelve 1500 x 3000 4881 and
+// 4722 (252).
 int tile_of(const int64_t* matrices, int n_mat)
 {
     double all = 0.0, large = 0.0, tiles = 0.0;
@@ -783,7 +777,7 @@ bool list_tiles(const int64_t* matrices, int n_mat, int k, Layout& L)
 }
 
 // matrices: {offset, rows, cols, stride} each.
-bool lay_out_all(const int64_t* matrices, int n_mat, bool split, Layout& L)
+bool lay_out_all(const int64_t* matrices, int n_mat, int type, Layout& L)
 {
     L.cuts = L.parts = 0;
     int64_t data = 0;
@@ -797,9 +791,9 @@ bool lay_out_all(const int64_t* matrices, int n_mat, bool split, Layout& L)
         if (!list_tiles(matrices, n_mat, k, L)) return false;
     for (int i = 0; i < n_mat; ++i) {
         Mat d;
-        data += lay_out(d, matrices[4 * i + 1], matrices[4 * i + 2], 0, split, L.tile);
+        data += lay_out(d, matrices[4 * i + 1], matrices[4 * i + 2], 0, L.tile);
         L.cuts += (uint64_t)(d.mp / CUT) * (uint64_t)(d.np / CUT);
-        L.parts += parts_of(matrices[4 * i + 1], matrices[4 * i + 2]);
+        L.parts += parts_of(matrices[4 * i + 1], matrices[4 * i + 2], type);
         if (L.cuts > MAX_TILES) return false;
     }
     int64_t at = 0;
@@ -873,32 +867,32 @@ constexpr double QUINTIC[3] = {3.4445, -4.7750, 2.0315};
 
 // Tiles of 128: two workgroups on a compute unit, one of which multiplies while the other starts or ends; A, whose sums are the
 // longest, has fewer tiles and takes one with twice the slabs under way (ResNet101 shape: 140 -> 97 us).
-template <Product PRODUCT, typename E, bool UPDATE, bool SPLIT>
+template <Product PRODUCT, typename E, bool UPDATE>
 void launch_product(const Call& p, const Layout& L, hipStream_t stream)
 {
     constexpr int K = PRODUCT == GRAM ? 0 : PRODUCT == POLY ? 1 : 2;
     const dim3 grid(DIES * L.list[K].longest);
-    if (L.side[K] == 256) hipLaunchKernelGGL((product_kernel<PRODUCT, SPLIT, E, UPDATE, 4, 4>), grid, dim3(256), 0, stream, p);
-    else if (L.side[K] == 128) hipLaunchKernelGGL((product_kernel<PRODUCT, SPLIT, E, UPDATE, 2, PRODUCT == GRAM ? 8 : 4>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((product_kernel<PRODUCT, SPLIT, E, UPDATE, 1, 8>), grid, dim3(256), 0, stream, p);
+    if (L.side[K] == 256) hipLaunchKernelGGL((product_kernel<PRODUCT, E, UPDATE, 4, 4>), grid, dim3(256), 0, stream, p);
+    else if (L.side[K] == 128) hipLaunchKernelGGL((product_kernel<PRODUCT, E, UPDATE, 2, PRODUCT == GRAM ? 8 : 4>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((product_kernel<PRODUCT, E, UPDATE, 1, 8>), grid, dim3(256), 0, stream, p);
 }
 
-template <typename E, bool UPDATE, bool SPLIT>
+template <typename E, bool UPDATE>
 void launch_products(Call& p, const Layout& L, int steps, const double* coefficients, hipStream_t stream)
 {
     for (int k = 0; k < steps; ++k) {
         const double* c = coefficients ? coefficients + 3 * k : QUINTIC;
         p.a = (float)c[0]; p.b = (float)c[1]; p.c = (float)c[2];
         p.flip = k & 1;
-        launch_product<GRAM, F32, false, SPLIT>(p, L, stream);
-        launch_product<POLY, F32, false, SPLIT>(p, L, stream);
-        if (k + 1 < steps) launch_product<NEXT, F32, false, SPLIT>(p, L, stream);
-        else launch_product<LAST, E, UPDATE, SPLIT>(p, L, stream);
+        launch_product<GRAM, F32, false>(p, L, stream);
+        launch_product<POLY, F32, false>(p, L, stream);
+        if (k + 1 < steps) launch_product<NEXT, F32, false>(p, L, stream);
+        else launch_product<LAST, E, UPDATE>(p, L, stream);
     }
 }
 
-template <typename E, bool UPDATE, bool SPLIT>
-int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, int n_mat, int steps, const double* coefficients,
+template <typename E, bool UPDATE>
+int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, int n_mat, int type, int steps, const double* coefficients,
         hipStream_t stream)
 {
     int64_t base = L.data;
@@ -906,7 +900,7 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
     for (int first = 0; first < n_mat; first += PER_INIT) {
         InitArgs a;
         std::memset(&a, 0, sizeof(a));
-        a.first = first; a.n = std::min(PER_INIT, n_mat - first); a.split = SPLIT; a.tile = L.tile;
+        a.first = first; a.n = std::min(PER_INIT, n_mat - first); a.tile = L.tile;
         for (int s = 0; s < 3; ++s) a.side[s] = L.side[s];
         for (int s = 0; s < 3; ++s) a.list[s] = L.list[s];
         for (int k = 0; k < a.n; ++k) {
@@ -916,20 +910,18 @@ int run(Call& p, const Layout& L, const int64_t* matrices, const float* scales, 
             g.stride = matrices[4 * i + 3];
             for (int s = 0; s < 3; ++s) g.tile[s] = L.first[s][i];
             Mat d;
-            g.base = base; base += lay_out(d, g.rows, g.cols, base, SPLIT, L.tile);
+            g.base = base; base += lay_out(d, g.rows, g.cols, base, L.tile);
             g.cut = cut; cut += (uint32_t)(d.mp / CUT) * (uint32_t)(d.np / CUT);
-            g.part = part; g.parts = (uint32_t)parts_of(g.rows, g.cols); part += g.parts;
+            g.part = part; g.parts = (uint32_t)parts_of(g.rows, g.cols, type); part += g.parts;
             g.scale = scales ? scales[i] : 1.0f;
         }
         hipLaunchKernelGGL(table_kernel, dim3((uint32_t)a.n), dim3(256), 0, stream, p, a);
     }
     hipLaunchKernelGGL((norm_kernel<E, UPDATE>), dim3((uint32_t)L.parts), dim3(256), 0, stream, p);
-    hipLaunchKernelGGL((cut_kernel<E, UPDATE, SPLIT>), dim3((uint32_t)L.cuts), dim3(256), 0, stream, p);
-    launch_products<E, UPDATE, SPLIT>(p, L, steps, coefficients, stream);
+    hipLaunchKernelGGL((cut_kernel<E, UPDATE>), dim3((uint32_t)L.cuts), dim3(256), 0, stream, p);
+    launch_products<E, UPDATE>(p, L, steps, coefficients, stream);
     return hipGetLastError() == hipSuccess ? GRAVAC_OK : GRAVAC_ERR_HIP;
 }
-
-bool in_two_parts(int type) { return type != GRAVAC_BFLOAT16; }
 
 // What both entry points check, and the parts of the call that are the same.
 int begin(Call& p, Layout& L, const int64_t* matrices, int n_mat, int type, int64_t n, int steps, const double* coefficients,
@@ -938,7 +930,7 @@ int begin(Call& p, Layout& L, const int64_t* matrices, int n_mat, int type, int6
     if (!known(type) || !matrices || n_mat < 1 || n_mat > MAX_MAT || n < 1 || n > MAX_FLAT) return GRAVAC_ERR_INVALID_ARG;
     if (steps < 1 || steps > GRAVAC_MAX_STEPS || !(eps >= 0.0) || std::isinf(eps)) return GRAVAC_ERR_INVALID_ARG;
     if (coefficients && !bounded(coefficients, steps)) return GRAVAC_ERR_INVALID_ARG;
-    if (!lay_out_all(matrices, n_mat, in_two_parts(type), L) || !lie_apart(matrices, n_mat, n)) return GRAVAC_ERR_INVALID_ARG;
+    if (!lay_out_all(matrices, n_mat, type, L) || !lie_apart(matrices, n_mat, n)) return GRAVAC_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < (size_t)L.total) return GRAVAC_ERR_WORKSPACE;
     std::memset(&p, 0, sizeof(p));
     p.ws = (char*)workspace;
@@ -967,7 +959,7 @@ int gravac_orthogonalize_workspace_bytes(const int64_t* matrices, int n_mat, int
 {
     Layout L;
     if (!bytes_out || !known(type) || !matrices || n_mat < 1 || n_mat > MAX_MAT ||
-        !lay_out_all(matrices, n_mat, in_two_parts(type), L))
+        !lay_out_all(matrices, n_mat, type, L))
         return GRAVAC_ERR_INVALID_ARG;
     *bytes_out = (size_t)L.total;
     return GRAVAC_OK;
@@ -983,9 +975,9 @@ int gravac_orthogonalize(const void* in, void* out, int type, int64_t n, const i
     if (in != out && overlap(in, n * size_of(type), out, n * size_of(type))) return GRAVAC_ERR_INVALID_ARG;
     p.in = in; p.out = out;
     hipStream_t stream = (hipStream_t)stream_v;
-    if (type == GRAVAC_FLOAT32) return run<F32, false, true>(p, L, matrices, nullptr, n_mat, steps, coefficients, stream);
-    if (type == GRAVAC_BFLOAT16) return run<BF16, false, false>(p, L, matrices, nullptr, n_mat, steps, coefficients, stream);
-    return run<F16, false, true>(p, L, matrices, nullptr, n_mat, steps, coefficients, stream);
+    if (type == GRAVAC_FLOAT32) return run<F32, false>(p, L, matrices, nullptr, n_mat, type, steps, coefficients, stream);
+    if (type == GRAVAC_BFLOAT16) return run<BF16, false>(p, L, matrices, nullptr, n_mat, type, steps, coefficients, stream);
+    return run<F16, false>(p, L, matrices, nullptr, n_mat, type, steps, coefficients, stream);
 }
 
 int gravac_orthogonal_update(const float* grad, float* momentum, void* params, int type, int64_t n, const int64_t* matrices,
@@ -1006,9 +998,9 @@ int gravac_orthogonal_update(const float* grad, float* momentum, void* params, i
     p.beta = beta; p.keep = keep; p.alpha = alpha;
     p.nesterov = (flags & GRAVAC_FLAG_NESTEROV) ? 1 : 0;
     hipStream_t stream = (hipStream_t)stream_v;
-    if (type == GRAVAC_FLOAT32) return run<F32, true, true>(p, L, matrices, scales, n_mat, steps, coefficients, stream);
-    if (type == GRAVAC_BFLOAT16) return run<BF16, true, false>(p, L, matrices, scales, n_mat, steps, coefficients, stream);
-    return run<F16, true, true>(p, L, matrices, scales, n_mat, steps, coefficients, stream);
+    if (type == GRAVAC_FLOAT32) return run<F32, true>(p, L, matrices, scales, n_mat, type, steps, coefficients, stream);
+    if (type == GRAVAC_BFLOAT16) return run<BF16, true>(p, L, matrices, scales, n_mat, type, steps, coefficients, stream);
+    return run<F16, true>(p, L, matrices, scales, n_mat, type, steps, coefficients, stream);
 }
 
 }  // extern "C"

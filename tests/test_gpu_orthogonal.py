@@ -372,3 +372,43 @@ def test_binding_refuses():
     assert e.value.code == B.ERR_WORKSPACE
     with pytest.raises(ValueError):
         B.Orthogonalizer(100, table)(torch.zeros(99, device="cuda"))
+
+
+# ---- the rounding to 16 bits ----------------------------------------------------------------------------------------
+
+def _beyond_rounding(got, want):
+    """How far entries of a 16-bit type are from the exact ones beyond half the spacing at them: an entry is the nearest one to
+    what was rounded, so this is at most what that was off by."""
+    bits, least = (8, -133) if got.dtype == torch.bfloat16 else (11, -24)
+    _, e = torch.frexp(got.double())
+    half = torch.ldexp(torch.ones((), dtype=torch.float64), torch.clamp(e - bits, min=least) - 1)
+    return (got.double() - want).abs().sub(half).clamp(min=0.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,cols", [(512, 128), (129, 128), (300, 1100), (1025, 515)])
+def test_16_bit_results_are_rounded_once(rows, cols, dtype):
+    """Before its rounding the result is as exact as one of float32: the tolerance is that of float32."""
+    for kind in ("normal", "low rank", "graded"):
+        G = _values(rows, cols, kind, rows + cols).to(dtype)
+        got = _orthogonalize(G.cuda().view(-1), [(0, rows, cols)]).cpu().view(rows, cols)
+        want = _exact(G)
+        err = float(torch.linalg.vector_norm(_beyond_rounding(got, want)) / torch.linalg.vector_norm(want))
+        bound = _tolerance(G, torch.float32)
+        print(rows, cols, dtype, kind, "error beyond the rounding %.2e of %.2e" % (err, bound))
+        assert err <= bound, kind
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_16_bit_parameters_take_the_direction_of_a_float32_momentum(dtype):
+    """The momentum is float32 whatever the parameters are, and so is its direction: parameters of zero become the step,
+    rounded once."""
+    r, c = 260, 384
+    mom = _values(r, c, "low rank", 19).view(-1).cuda()
+    params = torch.zeros(r * c, dtype=dtype, device="cuda")
+    U = mom.cpu().view(r, c)
+    B.Orthogonalizer(r * c, [(0, r, c)], dtype).update(torch.zeros(r * c, device="cuda"), mom, params, beta=1.0, alpha=-1.0)
+    want = -_exact(U)
+    err = torch.linalg.vector_norm(_beyond_rounding(params.cpu().view(r, c), want)) / torch.linalg.vector_norm(want)
+    # the direction, and the binary32 product and sum around it (each exact or half a step)
+    assert err <= _tolerance(U, torch.float32) + 2 * 2.0 ** -24
