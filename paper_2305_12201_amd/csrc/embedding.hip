@@ -150,7 +150,8 @@ __device__ __forceinline__ uint32_t key_at(const GradParams& p, int64_t i)
 
 // A workgroup clears the rows that no token names of a block of fill_rows (at most 64, about FILL_ELEMENTS elements): all of
 // its threads write consecutive places, and workgroups that run together neighbouring blocks.  (A wavefront per row, the
-// rows of a workgroup far apart or not, wrote 2 to 4.7 TB/s, this 5.8.)  absent: a bit per row of the block.
+// rows of a workgroup far apart or not, wrote 2 to 4.7 TB/s, this 5.8.)  absent: a bit per row of the block, which begins inside
+// the table.
 constexpr int64_t FILL_ELEMENTS = 16384;
 
 __device__ void clear_rows(const GradParams& p, int64_t row0, uint64_t absent)
@@ -420,20 +421,19 @@ __global__ __launch_bounds__(64 * SUM_W) void sum_kernel(GradParams p, int sorte
     const uint2* pairs = p.pairs[sorted];
     if (blockIdx.x < p.fills) {
         const int64_t id = (int64_t)blockIdx.x * gridDim.y + blockIdx.y, r = id * p.fill_rows + lane;
+        if (id >= p.fill_wgs) return;   // (the grid holds whole groups of gridDim.y: the last may go on behind the table)
         const uint32_t row = (uint32_t)r;
-        bool named = lane >= p.fill_rows || id >= p.fill_wgs || r >= p.vocab;
-        if (id < p.fill_wgs) {
-            uint32_t lo = first_at_least(pairs, (uint32_t)p.n, (uint32_t)(id * p.fill_rows));
-            uint32_t hi = first_at_least(pairs, (uint32_t)p.n, (uint32_t)(id * p.fill_rows) + p.fill_rows);
-            if (!named) {
-                const uint32_t behind = hi;
-                while (lo < hi) {
-                    const uint32_t mid = lo + (hi - lo) / 2;
-                    if (pairs[mid].x < row) lo = mid + 1;
-                    else hi = mid;
-                }
-                named = lo < behind && pairs[lo].x == row;
+        bool named = lane >= p.fill_rows || r >= p.vocab;
+        uint32_t lo = first_at_least(pairs, (uint32_t)p.n, (uint32_t)(id * p.fill_rows));
+        uint32_t hi = first_at_least(pairs, (uint32_t)p.n, (uint32_t)(id * p.fill_rows) + p.fill_rows);
+        if (!named) {
+            const uint32_t behind = hi;
+            while (lo < hi) {
+                const uint32_t mid = lo + (hi - lo) / 2;
+                if (pairs[mid].x < row) lo = mid + 1;
+                else hi = mid;
             }
+            named = lo < behind && pairs[lo].x == row;
         }
         clear_rows(p, id * p.fill_rows, ~__ballot(named));
         return;

@@ -352,3 +352,59 @@ def test_binding_refuses():
     assert e.value.code == B.ERR_WORKSPACE
     with pytest.raises(B.GravacError):
         B.gravac_embedding_gradient(out[:1].expand(3, 6), tokens, table, workspace=ws)     # rows one over the other
+
+
+def _wide_rows(dim, dtype):
+    """How many rows of a table a workgroup looks after (those that no token names), and how many workgroups share one group of
+    them, for more than 1024 tokens and a table without gaps: the sizes at which the last group is whole, or is not."""
+    n = 16 // torch.empty((), dtype=dtype).element_size()
+    slabs = -(-dim // (64 * n))
+    return max(1, min(64, 65536 // dim)), -(-slabs // min(slabs, 8))
+
+
+WIDE = [(2052, torch.float32), (2560, torch.float32), (4096, torch.float32), (4100, torch.float32), (8192, torch.bfloat16), (5120, torch.float16),
+        (40_000, torch.float32)]
+
+
+@pytest.mark.parametrize("dim,dtype", WIDE)
+def test_gradient_of_wide_rows(dim, dtype):
+    """Whole numbers, rows of several workgroups' columns, any number of blocks of rows, the last one whole or not."""
+    n = 1100
+    rows, columns = _wide_rows(dim, dtype)
+    g = torch.Generator().manual_seed(dim)
+    whole = torch.randint(-8, 9, (n, dim), generator=g).to(dtype)
+    grad_out = whole.cuda()
+    for blocks in range(2 * columns, 3 * columns + 1):
+        for vocab in {rows * blocks, max(rows * blocks - 3, rows * (blocks - 1) + 1)}:
+            tokens = _tokens(n, vocab, torch.int32, blocks, "padded")
+            tokens[tokens % 5 == 2] = -1                    # rows that no token names
+            ok = (tokens >= 0) & (tokens < vocab)
+            table = torch.full((vocab + 2, dim), 3.0, device="cuda")     # two rows behind it
+            _gradient(grad_out, tokens.cuda(), table[:vocab])
+            want = torch.zeros(vocab, dim, dtype=torch.float64).index_add_(0, tokens[ok].long(), whole[ok].double())
+            assert torch.equal(table[:vocab].cpu().double(), want), (blocks, vocab)
+            assert (table[vocab:] == 3.0).all()
+
+
+@pytest.mark.parametrize("dim,dtype", [(2560, torch.float32), (4096, torch.float32), (8192, torch.bfloat16)])
+def test_gradient_of_wide_rows_takes_as_long_for_any_number_of_blocks(dim, dtype):
+    """A table one block of rows larger costs no more than that block: workgroups that have no block end at once."""
+    n = 2000
+    rows, columns = _wide_rows(dim, dtype)
+    grad_out = torch.zeros(n, dim, dtype=dtype, device="cuda")
+    tokens = _tokens(n, 100, torch.int64, 1, "text").cuda()
+    took = []
+    for blocks in (40 * columns, 40 * columns + 1):
+        table = torch.empty(rows * blocks, dim, device="cuda")
+        ws = torch.empty(B.gravac_embedding_gradient_workspace_bytes(n, *table.shape), dtype=torch.uint8, device="cuda")
+        times = []
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            _gradient(grad_out, tokens, table, ws=ws)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        took.append(min(times))
+    print(dim, dtype, "ms with whole groups of blocks and with one more: %.3f %.3f" % tuple(took))
+    assert took[1] < 2 * took[0] + 0.5, took      # (a loop over 2^32 elements takes ten milliseconds and more)
