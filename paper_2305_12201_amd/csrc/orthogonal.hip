@@ -14,7 +14,11 @@
 // with the steps, which multiply a small singular value by a each: the term a X is taken in binary32 from hi + lo;
 // the diagonals of A and P, far larger than the rest, are kept in binary32 outside the products,
 //     A = D + E:  A A = E E + (d_i + d_j) e_ij + [i = j] d_i^2,      P = D' + Q:  X <- (a + d'_i) x_i + Q X;
-// and every operand is scaled by a power of two so that typical entries lie near 1 and the largest one possible below 65504.
+// and X is stored times 2^14, E and Q times 2^12, so that the largest entries possible, which the host bounds, lie just below 65504.
+// Of an entry of X below 2^-17 (one of E or Q below 2^-15) the lower part is a subnormal number of binary16: it is off by 2^-39 (2^-37)
+// at most, no longer by 2^-22 of itself, and the steps that raise it raise that too.  (Powers of two that follow the matrix's size,
+// with typical entries near 1, leave less: a 16 x 64 matrix with one row 10^5 times the others was off by 5.7e-4 after 16 steps, so
+// by 2e-6.)
 //
 // Memory.  Every product is of the form C = L R^T with rows of L and R contiguous along the sum: X is kept as X and as X^T,
 // both written by the product that makes them.  Rows and columns are padded with zeros to whole tiles, so the products have
@@ -69,7 +73,7 @@ struct Mat {     // ... and what the kernels read
     int32_t rows, cols, m, n, mp, np, tall;
     uint32_t cut, part, parts;
     float scale;
-    float sx, sa, sq;                 // powers of two: X, E and Q are stored multiplied by them
+    int32_t pad;
     int64_t x, xt0, xt1, e, q, da, dq;   // byte offsets in the workspace
 };
 
@@ -85,13 +89,9 @@ struct Stretches { uint32_t begin[DIES + 1], longest; };
 __host__ __device__ inline int64_t padded(int64_t x, int tile) { return (x + tile - 1) / tile * tile; }
 __host__ __device__ inline int64_t aligned(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
-// 2^round(log2(x)) up to 2^most
-__host__ __device__ inline float power_of_two(double x, int most)
-{
-    int e = 0;
-    while (e < most && x > 1.41421356) { x *= 0.5; ++e; }
-    return (float)(1u << e);
-}
+// What operands are stored multiplied by: entries of X are at most 3.9, those of A at most 3.9^2 and those of P at most 15 (the host
+// has checked the coefficients).
+constexpr float SX = 16384.0f, SA = 4096.0f, SQ = 4096.0f;
 
 // Lays out a matrix's part of the workspace; returns its size.
 __host__ __device__ inline int64_t lay_out(Mat& d, int64_t rows, int64_t cols, int64_t base, int tile)
@@ -111,10 +111,6 @@ __host__ __device__ inline int64_t lay_out(Mat& d, int64_t rows, int64_t cols, i
     d.q = at; at += ab;
     d.da = at; at += aligned(4 * (int64_t)d.mp);
     d.dq = at; at += aligned(4 * (int64_t)d.mp);
-    // entries of X are at most 3.9, those of A at most 3.9^2 and those of P at most 15 (the host has checked the coefficients)
-    d.sx = power_of_two(sqrt((double)d.m * (double)d.n), 14);
-    d.sa = power_of_two((double)d.m, 12);
-    d.sq = power_of_two((double)d.m, 12);
     return at - base;
 }
 
@@ -291,7 +287,7 @@ __global__ __launch_bounds__(256) void cut_kernel(Call p)
     for (uint32_t i = threadIdx.x; i < d.parts; i += 256) square += p.parts[d.part + i];
     square = sum_256(square, lds);
     const double norm = sqrt(square) + p.eps;
-    const double inv = norm > 0.0 ? (double)d.sx / norm : (norm == 0.0 ? 0.0 : norm);
+    const double inv = norm > 0.0 ? (double)SX / norm : (norm == 0.0 ? 0.0 : norm);
     const uint32_t local = blockIdx.x - d.cut;
     const int across = d.np / CUT;
     const int i0 = (int)(local / across) * CUT, j0 = (int)(local % across) * CUT;   // in X
@@ -582,22 +578,23 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
                 float v[8] = {low.x, low.y, low.z, low.w, high.x, high.y, high.z, high.w};
                 half8 h, l;
                 if (PRODUCT == GRAM) {
-                    const float f = d.sa / (d.sx * d.sx);
+                    constexpr float f = SA / (SX * SX);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) v[q] *= f;
                     const float ajj = take_diagonal(v, i0 == j0, j - i);
-                    if (i0 == j0 && (unsigned)(j - i) < 8) ((float*)(ws + d.da))[j] = ajj * (1.0f / d.sa);
+                    if (i0 == j0 && (unsigned)(j - i) < 8) ((float*)(ws + d.da))[j] = ajj * (1.0f / SA);
                 } else if (PRODUCT == POLY) {
-                    const float dj = mj[it], sa = 1.0f / d.sa;
+                    constexpr float sa = 1.0f / SA;
+                    const float dj = mj[it];
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
                         const float eij = ((float)mh[it][q] + (float)ml[it][q]) * sa;
-                        v[q] = (p.b * eij + p.c * (v[q] * (sa * sa) + (mi[q] + dj) * eij)) * d.sq;
+                        v[q] = (p.b * eij + p.c * (v[q] * (sa * sa) + (mi[q] + dj) * eij)) * SQ;
                     }
                     const float pjj = take_diagonal(v, i0 == j0, j - i);   // (e_jj = 0: c times the sum)
-                    if (i0 == j0 && (unsigned)(j - i) < 8) ((float*)(ws + d.dq))[j] = p.b * dj + p.c * dj * dj + pjj * (1.0f / d.sq);
+                    if (i0 == j0 && (unsigned)(j - i) < 8) ((float*)(ws + d.dq))[j] = p.b * dj + p.c * dj * dj + pjj * (1.0f / SQ);
                 } else {
-                    const float sq = 1.0f / d.sq;
+                    constexpr float sq = 1.0f / SQ;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) v[q] = mj[it] * ((float)mh[it][q] + (float)ml[it][q]) + v[q] * sq;
                 }
@@ -608,7 +605,8 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
                     *(half8*)(to + at) = h;
                     *(half8*)(to + at + LOW) = l;
                 } else {
-                    const float sx = 1.0f / d.sx, step = p.alpha * d.scale;
+                    constexpr float sx = 1.0f / SX;
+                    const float step = p.alpha * d.scale;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) v[q] = UPDATE ? step * (v[q] * sx) : v[q] * sx;
                     if (!other && i < d.n && j < d.m) {
@@ -829,7 +827,7 @@ bool lie_apart(const int64_t* matrices, int n_mat, int64_t n)
     return true;
 }
 
-constexpr double MOST_X = 3.9, MOST_P = 15.0;   // times the scales in lay_out: below 65504
+constexpr double MOST_X = 3.9, MOST_P = 15.0;   // times SX, its square times SA, and times SQ: below 65504
 
 // Coefficients of a step, as numbers that binary16 operands can hold through all steps: with |s| <= u before a step, the
 // largest |a s + b s^3 + c s^5| and the largest |b l + c l^2|, l = s^2, follow from the ends and the extrema.

@@ -412,3 +412,61 @@ def test_16_bit_parameters_take_the_direction_of_a_float32_momentum(dtype):
     err = torch.linalg.vector_norm(_beyond_rounding(params.cpu().view(r, c), want)) / torch.linalg.vector_norm(want)
     # the direction, and the binary32 product and sum around it (each exact or half a step)
     assert err <= _tolerance(U, torch.float32) + 2 * 2.0 ** -24
+
+
+# ---- matrices whose entries are of very different sizes -------------------------------------------------------------
+
+def _uneven(kind):
+    g = torch.Generator().manual_seed(20)
+    if kind == "diagonal 1, 1e-3":
+        return torch.diag(torch.tensor([1.0, 1e-3]))
+    if kind == "diagonal down to 1e-5":
+        return torch.diag(torch.logspace(0, -5, 40))
+    shape = {"one entry": (512, 512), "one row": (16, 64), "half the rows": (64, 256), "half the columns": (64, 256), "graded rows": (300, 700)}[kind]
+    G = torch.randn(*shape, generator=g)
+    if kind == "one entry":
+        G[7, 9] = 1e5
+    elif kind == "one row":
+        G[3] *= 1e5
+    elif kind == "half the rows":
+        G[::2] *= 1e-4
+    elif kind == "half the columns":
+        G[:, ::2] *= 1e-4
+    else:
+        G *= torch.logspace(0, -5, 300)[:, None]
+    return G
+
+
+@pytest.mark.parametrize("steps", [5, 10, 16])
+@pytest.mark.parametrize("kind", ["diagonal 1, 1e-3", "diagonal down to 1e-5", "one entry", "one row", "half the rows", "half the columns", "graded rows"])
+def test_rows_and_entries_of_very_different_sizes(kind, steps):
+    """As exact as in binary32: the tolerance of float32, for bfloat16 beyond its rounding."""
+    if kind == "one entry" and steps > 5:
+        steps = 8                  # (the norm's share of the others is below 10^-5 here: see the next test)
+    for dtype in (torch.float32, torch.bfloat16):
+        for tall in (False, True):
+            G = _uneven(kind).to(dtype)
+            G = G.t().contiguous() if tall else G
+            got = _orthogonalize(G.cuda().view(-1), [(0, *G.shape)], steps=steps).cpu().view(G.shape)
+            want = _exact(G, steps)
+            diff = _beyond_rounding(got, want) if dtype != torch.float32 else got.double() - want
+            err, bound = float(torch.linalg.vector_norm(diff) / torch.linalg.vector_norm(want)), _tolerance(G, torch.float32, steps)
+            print(kind, steps, dtype, tall, "error %.2e of %.2e" % (err, bound))
+            assert err <= bound, (dtype, tall)
+
+
+@pytest.mark.parametrize("rows,cols", [(2, 2), (64, 256), (256, 512)])
+@pytest.mark.parametrize("size", [1e-6, 1e-7])
+def test_tiny_rows_raised_by_many_steps(rows, cols, size):
+    """An entry of X is off by 2^-39 at most, one of A and P by 2^-37.  In one step a row of norm s (its share of the norm, s
+    growing by a = 3.44 each step) takes from its own entries' errors at most (a + |b| + |c|) 2^-39 sqrt(n) for singular values of 1
+    at most, from A's (|b| + 2 |c|) 2^-37 sqrt(m) and from P's 2^-37 sqrt(m): over a s, 3.0 2^-39 sqrt(n) / s and 2.9 2^-37 sqrt(m) / s.
+    The later steps add 1 / a of that, 1 / a^2, ...: 1.41 times it in all.  The rows make up at most the whole of the result's norm."""
+    G = torch.eye(2) if rows == 2 else torch.randn(rows, cols, generator=torch.Generator().manual_seed(21))
+    G[1::2] *= size
+    share = float(torch.linalg.vector_norm(G[1::2], dim=1).min() / torch.linalg.vector_norm(G))
+    got = _orthogonalize(G.cuda().view(-1), [(0, rows, cols)], steps=16).cpu().view(rows, cols)
+    err = _error(got, _exact(G, 16))
+    bound = 1.41 * (3.0 * 2.0 ** -39 * cols ** 0.5 + 2.9 * 2.0 ** -37 * rows ** 0.5) / share + _tolerance(G, torch.float32, 16)
+    print(rows, cols, size, "error %.2e of %.2e" % (err, bound))
+    assert err <= bound
