@@ -370,7 +370,9 @@ int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tok
  * Another step in the place of w - eta * g~ of Alg. 1, for parameters that are matrices: the momentum of the aggregated
  * gradient with its singular values made equal, by Newton-Schulz products.  A matrix U becomes O by
  *     X = U / (||U||_F + eps),   steps times   X <- a X + b (X X^T) X + c (X X^T)^2 X,   O = X
- * (for more rows than columns with X^T X from the right, which is the same), whose products run on the matrix cores.
+ * (for more rows than columns with X^T X from the right, which is the same), whose products run on the matrix cores.  The order
+ * of their sums follows from the call's table alone, so a call repeats itself bit for bit; a matrix with a side beyond 2048 can
+ * differ in its last bits from what it is in a call with other matrices, which may take other tiles.
  *
  *   matrices        host, int64[n_mat][4], 1 <= n_mat <= GRAVAC_MAX_MATRICES: offset of the first element in the flat
  *                   vector, rows, columns, elements from one row to the next (>= columns).  Rows and columns 1 .. 2^20, the

@@ -48,7 +48,7 @@ typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr int SLAB = 64;           // bytes of an operand's row that are fetched at a time: 16 elements as hi and lo
-constexpr int PART_SLABS = 128;    // slabs of a sum that are added one after the other (tiles of 128)
+constexpr int PART_SLABS = 128;    // slabs of a sum that are added one after the other (tiles of 64 and 128)
 constexpr int64_t LONG_SIDE = 32768;   // no tiles of 256 for longer sums
 constexpr int BLOCK = 128;         // rows whose slabs stand together in memory
 constexpr int MAX_MAT = GRAVAC_MAX_MATRICES;
@@ -456,7 +456,9 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
     // busy 61 % of the time).
     constexpr int PRODUCTS = 3, INSTS = PRODUCTS * F * F, ITEMS = 6 * F;
     // A long sum is added up in parts: added one after the other, 70,001 elements of float32 are off by 16 times what the
-    // plain evaluation's nested sums are.  (There are no registers for that with tiles of 256, which longer sums do not get.)
+    // plain evaluation's nested sums are.  There are no registers for that with tiles of 256, which sums beyond LONG_SIDE do not get:
+    // 32,768 elements added one after the other are off by twice to three times what nested sums are, random ones and ones of one
+    // sign (1024 x 20,011 2.0e-6 and 3.6e-6, a nested evaluation in binary32 1.4e-6 and 1.6e-6).
     constexpr bool PARTS = F <= 2;
     float16v sums[PARTS ? F : 1][PARTS ? F : 1];
     auto add_up = [&](bool first) {
@@ -514,8 +516,9 @@ __global__ __launch_bounds__(256, F == 4 || (F == 2 && BUFFERS > 4) ? 1 : 2) voi
 #pragma unroll
         for (int bj = 0; bj < BLOCKS; ++bj) {
             const int i0 = t.i * T + wi + bi * SIDE, j0 = t.j * T + wj + bj * SIDE;
-            // A symmetric matrix takes its upper half from the lower one, in units of 32 whatever the tiles are: so the result
-            // does not depend on them (the parts of a product are added in another order on the other side).
+            // A symmetric matrix takes its upper half from the lower one, in units of 32 whatever the tiles are (the parts of a
+            // product are added in another order on the other side): so the result depends on the tiles only where sums are folded,
+            // beyond PART_SLABS slabs, and the tile is 256, which the other matrices of the call decide too.
             constexpr bool SYMMETRIC = PRODUCT == GRAM || PRODUCT == POLY;
             if (SYMMETRIC && i0 < j0) continue;
             const int part = (lane % EIGHTS) * 8, column = lane / EIGHTS, i = i0 + part;

@@ -470,3 +470,35 @@ def test_tiny_rows_raised_by_many_steps(rows, cols, size):
     bound = 1.41 * (3.0 * 2.0 ** -39 * cols ** 0.5 + 2.9 * 2.0 ** -37 * rows ** 0.5) / share + _tolerance(G, torch.float32, 16)
     print(rows, cols, size, "error %.2e of %.2e" % (err, bound))
     assert err <= bound
+
+
+# ---- the larger tiles -----------------------------------------------------------------------------------------------
+
+def _gpu_tolerance(G, dtype):
+    """_tolerance's for float32 and float16, on the GPU."""
+    return 12 * _error(_exact(G, dtype=torch.float32), _exact(G)) + 2.0 ** -22 + (HALF_STEP[dtype] if dtype != torch.float32 else 0.0)
+
+
+@pytest.mark.parametrize("kind", ["normal", "one sign", "low rank"])
+def test_long_sums_in_tiles_of_256(kind):
+    """Sums of up to 32,768 elements, the longest that tiles of 256 are used for; those of one sign are the hardest to add up.  The
+    plain evaluation that the tolerance is made from adds up in binary32 too, in no more nested an order than a library's."""
+    shapes = [(1024, 32_768), (31_999, 1100), (2048, 30_000), (1024, 20_011), (1500, 25_088), (32_768, 2048)]   # 128 tiles of A
+    at, matrices = 0, []
+    for r, c in shapes:
+        matrices.append((at, r, c))
+        at += r * c
+    g = torch.Generator(device="cuda").manual_seed(22)
+    x = torch.randn(at, device="cuda", generator=g)
+    if kind == "one sign":
+        x.abs_()
+    elif kind == "low rank":
+        for off, r, c in matrices:
+            u, v = torch.randn(r, 3, device="cuda", generator=g), torch.randn(3, c, device="cuda", generator=g)
+            x[off:off + r * c] = (u @ v).view(-1) + 0.1 * x[off:off + r * c]
+    got = _orthogonalize(x, matrices)
+    for off, r, c in matrices:
+        G = x[off:off + r * c].view(r, c)
+        err, bound = _error(got[off:off + r * c].view(r, c), _exact(G)), _gpu_tolerance(G, torch.float32)
+        print(kind, r, c, "error %.2e of %.2e" % (err, bound))
+        assert err <= bound, (r, c)
