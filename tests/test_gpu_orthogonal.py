@@ -502,3 +502,56 @@ def test_long_sums_in_tiles_of_256(kind):
         err, bound = _error(got[off:off + r * c].view(r, c), _exact(G)), _gpu_tolerance(G, torch.float32)
         print(kind, r, c, "error %.2e of %.2e" % (err, bound))
         assert err <= bound, (r, c)
+
+
+# Tables by the sides of the tiles of A, P and X that their sizes lead to: wide, tall, ragged and small matrices together.
+LARGE = {
+    "128, 64, 128": [(1700, 2100), (2100, 1700), (300, 65), (1, 40), (128, 1000)],
+    "128, 128, 128": [(700, 760), (760, 690)] * 13 + [(33, 70)],
+    "256, 256, 256": [(1300, 1290), (1290, 1411), (1411, 1300)] * 3 + [(60, 90), (7, 1)],
+    "256, 128, 256": [(1025, 2100), (2100, 1027), (1040, 2049)] * 3 + [(60, 90), (1, 300)],
+}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("sides", LARGE)
+def test_update_in_larger_tiles(sides, nesterov, dtype):
+    """orthogonalize and update of tables that take tiles of 128 and of 256, every third matrix with gaps between its rows; 64 bits
+    on the GPU."""
+    at, matrices = 3, []
+    for r, c in LARGE[sides]:
+        stride = c + (5 if len(matrices) % 3 == 1 else 0)
+        matrices.append((at, r, c, stride))
+        at += r * stride + 7
+    g = torch.Generator(device="cuda").manual_seed(23)
+    rand = lambda s: torch.randn(at, device="cuda", generator=g) * s  # noqa: E731
+    view = lambda x, m: x.as_strided((m[1], m[2]), (m[3], 1), m[0])  # noqa: E731
+    inside = torch.zeros(at, dtype=torch.bool, device="cuda")
+    for m in matrices:
+        view(inside, m).fill_(True)
+    x = rand(1.0).to(dtype)
+    out = _orthogonalize(x, matrices, out=torch.full((at,), 7.0, dtype=dtype, device="cuda"))
+    assert (out[~inside] == 7.0).all()
+    grad, mom, params = rand(1e-3), rand(1e-2), rand(0.02).to(dtype)
+    m0, p0 = mom.clone(), params.clone()
+    beta, keep, alpha = 0.95, 0.99, -0.02
+    f = lambda v: np.float32(v).item()  # noqa: E731
+    scales = [0.2 * max(r, c) ** 0.5 for r, c in LARGE[sides]]
+    B.Orthogonalizer(at, matrices, dtype).update(grad, mom, params, beta=beta, alpha=alpha, keep=keep, nesterov=nesterov, scales=scales)
+    new = m0 * f(beta) + grad
+    assert torch.equal(mom, torch.where(inside, new, m0)) and torch.equal(params[~inside], p0[~inside])
+    U = grad + f(beta) * new if nesterov else new
+    for i, m in enumerate(matrices):
+        if i > 2 and i + 3 < len(matrices):
+            continue                     # (of the same shapes as others)
+        want = _exact(view(x, m))
+        assert _error(view(out, m), want) <= _gpu_tolerance(view(x, m), dtype), m
+        O, old = _exact(view(U, m)), view(p0, m).double()
+        step = f(f(alpha) * f(scales[i]))
+        want = f(keep) * old + step * O
+        err = torch.linalg.vector_norm(view(params, m).double() - want)
+        # the direction; two binary32 products and their sum; one rounding to the type
+        bound = abs(step) * _gpu_tolerance(view(U, m), torch.float32) * torch.linalg.vector_norm(O) + \
+            (HALF_STEP[dtype] + 3 * 2.0 ** -24) * torch.linalg.vector_norm(want.abs() + old.abs())
+        assert err <= bound, (m, float(err), float(bound))
