@@ -335,7 +335,8 @@ int gravac_decompress_accumulate_static(const int32_t* idx, const float* val,
  * token outside [0, vocab) (a padded place) gives a row of +0.
  *
  *   table           device, table_type[vocab][table_stride], read only.
- *   out             device, out_type[n_tokens][out_stride]; must not overlap the table.
+ *   out             device, out_type[n_tokens][out_stride]; shares no element with the table or the tokens (refused; the rows
+ *                   of one may lie between those of the other).
  */
 int gravac_embedding_lookup(const void* table, int table_type, int64_t vocab, int64_t dim, int64_t table_stride,
                             const void* tokens, int token_bytes, int64_t n_tokens, float scale,
@@ -353,9 +354,10 @@ int gravac_embedding_lookup(const void* table, int table_type, int64_t vocab, in
  *   grad_out        device, grad_type[n_tokens][grad_stride], read only.
  *   padding_token   positions with this token take no part, and neither do tokens outside [0, vocab).  Any value outside
  *                   [0, vocab), such as -1, if there is no such token.
- *   table_grad      device, float[vocab][table_stride]; must not overlap grad_out.
+ *   table_grad      device, float[vocab][table_stride]; shares no element with grad_out or the tokens (refused).
  *   workspace       device, 256-byte aligned, at least gravac_embedding_gradient_workspace_bytes(n_tokens, vocab, dim)
- *                   bytes: 16 per token, and two rows of partial sums per 4 to 32 tokens.
+ *                   bytes: 16 per token, and two rows of partial sums per 4 to 32 tokens.  Apart from the other buffers
+ *                   (refused).
  *   flags           0 or GRAVAC_FLAG_ACCUMULATE.
  */
 int gravac_embedding_gradient_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, size_t* bytes_out);

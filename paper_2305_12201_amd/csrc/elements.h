@@ -19,6 +19,38 @@ struct F16 { using word = uint16_t; static constexpr int SIZE = 2; };
 inline bool known(int type) { return type == GRAVAC_FLOAT32 || type == GRAVAC_BFLOAT16 || type == GRAVAC_FLOAT16; }
 inline int size_of(int type) { return type == GRAVAC_FLOAT32 ? 4 : 2; }
 
+// Rows of `length` that begin `stride` >= length apart; bytes or elements.
+struct Rows { int64_t begin, rows, length, stride; };
+
+// Whether two of them share anything.
+inline bool share(const Rows& x, const Rows& y)
+{
+    typedef __int128 wide;
+    if (x.rows < 1 || y.rows < 1) return false;
+    const Rows &a = x.rows < y.rows ? y : x, &b = x.rows < y.rows ? x : y;   // b: the one with fewer rows
+    const wide d = (wide)b.begin - a.begin;
+    if (d >= (wide)(a.rows - 1) * a.stride + a.length || -d >= (wide)(b.rows - 1) * b.stride + b.length) return false;
+    auto floor_of = [](wide p, wide q) { return p / q - (p % q < 0 ? 1 : 0); };
+    if (a.stride == b.stride) {
+        // a row of b begins d + k stride behind one of a, k = 1 - a.rows .. b.rows - 1: the first of these behind -b.length
+        const wide k = floor_of(-(wide)b.length - d, a.stride) + 1, first = k < 1 - (wide)a.rows ? 1 - (wide)a.rows : k;
+        return first < b.rows && d + first * a.stride < a.length;
+    }
+    for (int64_t j = 0; j < b.rows; ++j) {
+        const wide at = d + (wide)j * b.stride;
+        wide i = floor_of(at + b.length - 1, a.stride);   // the last row of a that begins before b's ends
+        if (i >= a.rows) i = a.rows - 1;
+        if (i >= 0 && i * a.stride + a.length > at) return true;
+    }
+    return false;
+}
+
+inline Rows rows_at(const void* p, int64_t rows, int64_t length, int64_t stride, int size)   // in bytes
+{
+    return {(int64_t)(uintptr_t)p, rows, length * size, stride * size};
+}
+inline Rows bytes_at(const void* p, int64_t bytes) { return {(int64_t)(uintptr_t)p, bytes > 0 ? 1 : 0, bytes, bytes}; }
+
 template <typename E> __device__ __forceinline__ float to_float(typename E::word w);
 template <> __device__ __forceinline__ float to_float<F32>(uint32_t w) { return __uint_as_float(w); }
 template <> __device__ __forceinline__ float to_float<BF16>(uint16_t w) { return __uint_as_float((uint32_t)w << 16); }

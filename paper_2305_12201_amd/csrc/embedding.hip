@@ -797,6 +797,9 @@ int gravac_embedding_lookup(const void* table, int table_type, int64_t vocab, in
     if (!table || misaligned(table, size_of(table_type))) return GRAVAC_ERR_INVALID_ARG;
     if (n_tokens == 0) return GRAVAC_OK;
     if (!tokens || !out || misaligned(tokens, token_bytes) || misaligned(out, size_of(out_type))) return GRAVAC_ERR_INVALID_ARG;
+    const Rows written = rows_at(out, n_tokens, dim, out_stride, size_of(out_type));
+    if (share(written, rows_at(table, vocab, dim, table_stride, size_of(table_type))) || share(written, bytes_at(tokens, n_tokens * token_bytes)))
+        return GRAVAC_ERR_INVALID_ARG;
     (void)hipGetLastError();
     LookupParams p;
     p.table = table; p.tokens = tokens; p.out = out;
@@ -832,6 +835,10 @@ int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tok
         return GRAVAC_ERR_INVALID_ARG;
     const GradLayout L = grad_layout(n_tokens, dim);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < L.total) return GRAVAC_ERR_WORKSPACE;
+    const Rows written = rows_at(table_grad, vocab, dim, table_stride, 4), scratch = bytes_at(workspace, (int64_t)L.total);
+    const Rows read[2] = {rows_at(grad_out, n_tokens, dim, grad_stride, size_of(grad_type)), bytes_at(tokens, n_tokens * token_bytes)};
+    if (share(written, scratch) || share(written, read[0]) || share(written, read[1]) || share(scratch, read[0]) || share(scratch, read[1]))
+        return GRAVAC_ERR_INVALID_ARG;
     (void)hipGetLastError();
     char* ws = (char*)workspace;
     GradParams p;

@@ -73,3 +73,25 @@ def test_binding_refuses_host_tensors():
         pytest.skip("the binding asks for the current device first")
     with pytest.raises(Exception):
         B.gravac_embedding_lookup(torch.zeros(4, 4), torch.zeros(2, dtype=torch.int64), torch.zeros(2, 4))
+
+
+# ---- buffers that share memory --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("bad", [
+    {"out": 0x1000}, {"out": 0x1000 + 6400 - 4}, {"out": 0x1000 - 252},                       # 100 rows of 64 bytes, 4 of 64
+    {"out": 0x1000 - 126, "out_type": B.BFLOAT16},
+    {"table_stride": 40, "out": 0x1000 + 60, "out_stride": 40},                              # the last element of the row
+    {"table_stride": 40, "out": 0x1000 + 100, "out_stride": 41},                             # ends in the next row
+    {"table_stride": 40, "out": 0x1000 + 64, "out_stride": 50},                              # its second row lies in a row of the table
+    {"table": 0x100000, "out": 0x2000}, {"table": 0x100000, "out": 0x201C}, {"table": 0x100000, "out": 0x2000 - 252},        # the tokens
+    {"table": 0x100000, "out": 0x2000 - 60, "out_stride": 1 << 20}])
+def test_lookup_refuses_shared_memory(bad):
+    assert _lookup(**{"n": 4, **bad}) == B.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("bad", [
+    {"grad": 0x3000}, {"grad": 0x3000 + 6396}, {"grad": 0x3000 - 636}, {"grad": 0x3000 - 318, "grad_type": B.FLOAT16},
+    {"table_stride": 40, "grad": 0x3000 + 60, "grad_stride": 40}, {"tokens": 0x3000}, {"tokens": 0x3000 - 72}, {"tokens": 0x4900 - 8},
+    {"ws": 0x1000}, {"ws": 0x1200}, {"ws": 0x2000}, {"ws": 0x3000}, {"ws": 0x4800}, {"grad": 0x10000}, {"tokens": 0x10008}, {"table": 0x10000 + 4},
+    {"table": 0x10000 - 6396}])
+def test_gradient_refuses_shared_memory(bad):
+    assert _gradient(**bad) == B.ERR_INVALID_ARG

@@ -408,3 +408,31 @@ def test_gradient_of_wide_rows_takes_as_long_for_any_number_of_blocks(dim, dtype
         took.append(min(times))
     print(dim, dtype, "ms with whole groups of blocks and with one more: %.3f %.3f" % tuple(took))
     assert took[1] < 2 * took[0] + 0.5, took      # (a loop over 2^32 elements takes ten milliseconds and more)
+
+
+def test_rows_of_two_buffers_that_lie_between_each_other():
+    """Two matrices in the columns of one buffer share no element, whatever their spans do: equal strides and one twice the other."""
+    vocab, dim, n = 40, 30, 80
+    buf = torch.full((2 * vocab * 100,), 7.0, device="cuda")
+    table, out = buf.view(vocab, 200)[:, 10:10 + dim], buf.view(n, 100)[:, 50:50 + dim]       # rows 200 and 100 apart
+    weights = torch.randn(vocab, dim, generator=torch.Generator().manual_seed(1))
+    table.copy_(weights)
+    tokens = _tokens(n, vocab, torch.int64, 2, "padded")
+    B.gravac_embedding_lookup(table, tokens.cuda(), out, scale=2.0)
+    want = _expected_lookup(weights, tokens, 2.0, torch.float32)
+    assert torch.equal(out.cpu(), want) and torch.equal(table.cpu(), weights)
+    with pytest.raises(B.GravacError) as e:
+        B.gravac_embedding_lookup(table, tokens.cuda(), buf.view(n, 100)[:, 39:39 + dim])
+    assert e.value.code == B.ERR_INVALID_ARG
+    # the gradient: both rows 100 apart
+    grad_out, sums = buf.view(n, 100)[:, :dim], buf.view(n, 100)[:vocab, dim:2 * dim]
+    grad_out.copy_(want)
+    for kw in ({}, {"accumulate": True}):
+        sums.fill_(1.0)
+        _gradient(grad_out, tokens.cuda(), sums, **kw)
+        total, size, count = _expected_gradient(want, tokens, vocab, -1, 1.0)
+        _check(sums.cpu(), total, size, count, torch.ones(vocab, dim) if kw else None)
+        assert torch.equal(grad_out.cpu(), want)
+    with pytest.raises(B.GravacError) as e:
+        _gradient(grad_out, tokens.cuda(), buf.view(n, 100)[:vocab, dim - 1:2 * dim - 1])
+    assert e.value.code == B.ERR_INVALID_ARG
