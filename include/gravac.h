@@ -396,7 +396,7 @@ int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tok
  *                   NaN in all of its elements and changes no other matrix.
  *   workspace       device, 256-byte aligned, at least gravac_orthogonalize_workspace_bytes(matrices, n_mat, type) bytes:
  *                   about 12 per element of the matrices, sides rounded up to whole tiles, and 8 per element of a square of
- *                   the smaller side.
+ *                   the smaller side.  Apart from the vectors (refused).
  *
  * The calls consist of kernel launches only and can be recorded into a graph; the host tables are read at capture time.
  */
@@ -408,7 +408,7 @@ int gravac_orthogonalize_workspace_bytes(const int64_t* matrices, int n_mat, int
 
 /*
  * out = O of the matrices of in.  Both are flat vectors of the same layout; out may be in itself, and must not overlap it
- * otherwise.
+ * otherwise (refused).
  */
 int gravac_orthogonalize(const void* in, void* out, int type, int64_t n, const int64_t* matrices, int n_mat,
                          int steps, const double* coefficients, double eps,
@@ -427,7 +427,7 @@ int gravac_orthogonalize(const void* in, void* out, int type, int64_t n, const i
  *   params          device, type[n], updated in place (the sum is rounded once to type).
  *   scales          host, float[n_mat], or NULL for 1: the step of each matrix, such as 0.2 sqrt(max(rows, columns)).
  *   flags           0 or GRAVAC_FLAG_NESTEROV.
- * The three vectors must not overlap.
+ * The three vectors must not overlap (refused).
  */
 int gravac_orthogonal_update(const float* grad, float* momentum, void* params, int type, int64_t n,
                              const int64_t* matrices, int n_mat, float beta, float keep, float alpha, const float* scales,

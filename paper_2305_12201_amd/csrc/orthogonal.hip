@@ -947,10 +947,7 @@ int begin(Call& p, Layout& L, const int64_t* matrices, int n_mat, int type, int6
 
 bool misaligned(const void* p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) != 0; }
 
-bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
-{
-    return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
-}
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) { return share(bytes_at(a, a_bytes), bytes_at(b, b_bytes)); }
 
 }  // namespace
 
@@ -973,7 +970,9 @@ int gravac_orthogonalize(const void* in, void* out, int type, int64_t n, const i
     Call p;
     Layout L;
     if (const int rc = begin(p, L, matrices, n_mat, type, n, steps, coefficients, eps, workspace, workspace_bytes)) return rc;
-    if (in != out && overlap(in, n * size_of(type), out, n * size_of(type))) return GRAVAC_ERR_INVALID_ARG;
+    const int64_t bytes = n * size_of(type);
+    if ((in != out && overlap(in, bytes, out, bytes)) || overlap(workspace, L.total, in, bytes) || overlap(workspace, L.total, out, bytes))
+        return GRAVAC_ERR_INVALID_ARG;
     p.in = in; p.out = out;
     hipStream_t stream = (hipStream_t)stream_v;
     if (type == GRAVAC_FLOAT32) return run<F32, false>(p, L, matrices, nullptr, n_mat, type, steps, coefficients, stream);
@@ -993,7 +992,8 @@ int gravac_orthogonal_update(const float* grad, float* momentum, void* params, i
     Layout L;
     if (const int rc = begin(p, L, matrices, n_mat, type, n, steps, coefficients, eps, workspace, workspace_bytes)) return rc;
     if (overlap(grad, 4 * n, momentum, 4 * n) || overlap(grad, 4 * n, params, n * size_of(type)) ||
-        overlap(momentum, 4 * n, params, n * size_of(type)))
+        overlap(momentum, 4 * n, params, n * size_of(type)) || overlap(workspace, L.total, grad, 4 * n) ||
+        overlap(workspace, L.total, momentum, 4 * n) || overlap(workspace, L.total, params, n * size_of(type)))
         return GRAVAC_ERR_INVALID_ARG;
     p.grad = grad; p.momentum = momentum; p.out = params;
     p.beta = beta; p.keep = keep; p.alpha = alpha;

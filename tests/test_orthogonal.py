@@ -124,3 +124,12 @@ def test_workspace_bytes():
         assert e.value.code == B.ERR_INVALID_ARG
     with pytest.raises(ValueError):
         size([(0, 1)])
+
+
+def test_refuses_workspaces_in_the_vectors():
+    need = B.gravac_orthogonalize_workspace_bytes(TABLE)
+    assert need > 0x1000
+    for bad in ({"x": 0x10000}, {"out": 0x10000}, {"x": 0x10000 - 3996}, {"out": 0x10000 + (need - 4) // 4 * 4}, {"x": 0x10800, "out": 0x10800}):
+        assert _orthogonalize(**bad) == B.ERR_INVALID_ARG
+    for bad in ({"grad": 0x10000}, {"momentum": 0x10000 - 3996}, {"params": 0x10000 + (need - 4) // 4 * 4}, {"params": 0x10000 - 1998, "type": B.BFLOAT16}):
+        assert _update(**bad) == B.ERR_INVALID_ARG
