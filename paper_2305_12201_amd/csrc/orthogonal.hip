@@ -821,11 +821,8 @@ bool lie_apart(const int64_t* matrices, int n_mat, int64_t n)
     std::sort(order, order + n_mat, [&](int a, int b) { return matrices[4 * a] < matrices[4 * b]; });
     for (int i = 0; i < n_mat; ++i)
         for (int k = i + 1; k < n_mat && matrices[4 * order[k]] < end(order[i]); ++k) {
-            // spans that overlap: only columns of one larger matrix lie apart (equal strides, and no columns in common)
             const int64_t *a = matrices + 4 * order[i], *b = matrices + 4 * order[k];
-            if (a[3] != b[3]) return false;
-            const int64_t d = (b[0] - a[0]) % a[3];   // b's first column, counted from a's
-            if (d < a[2] || d + b[2] > a[3]) return false;
+            if (share({a[0], a[1], a[2], a[3]}, {b[0], b[1], b[2], b[3]})) return false;
         }
     return true;
 }

@@ -133,3 +133,29 @@ def test_refuses_workspaces_in_the_vectors():
         assert _orthogonalize(**bad) == B.ERR_INVALID_ARG
     for bad in ({"grad": 0x10000}, {"momentum": 0x10000 - 3996}, {"params": 0x10000 + (need - 4) // 4 * 4}, {"params": 0x10000 - 1998, "type": B.BFLOAT16}):
         assert _update(**bad) == B.ERR_INVALID_ARG
+
+
+def test_tables_are_refused_exactly_where_elements_are_shared():
+    """Small tables in any order, of any strides, against sets of elements."""
+    rng = np.random.default_rng(5)
+    apart = 0
+    for _ in range(4000):
+        n, table, seen, ok = 70, [], set(), True
+        for _ in range(int(rng.integers(2, 4))):
+            rows, cols = int(rng.integers(1, 6)), int(rng.integers(1, 5))
+            table.append((int(rng.integers(0, 30)), rows, cols, cols + int(rng.integers(0, 12))))
+        for off, rows, cols, stride in table:
+            mine = {off + i * stride + j for i in range(rows) for j in range(cols)}
+            ok = ok and max(mine) < n and not (mine & seen)
+            seen |= mine
+        # (an allowed table goes on to the workspace's check)
+        assert _orthogonalize(matrices=table, n=n, ws=0) == (B.ERR_WORKSPACE if ok else B.ERR_INVALID_ARG), table
+        apart += ok
+    assert 200 < apart < 3800
+
+
+def test_tables_of_different_strides_lie_apart():
+    # one row between two others; two row lengths of the same buffer; long ones
+    for table in ([(0, 10, 8, 20), (8, 1, 12, 12)], [(0, 10, 8, 20), (28, 4, 8, 40)], [(0, 1 << 20, 1, 1 << 19), (1, 1 << 18, 7, 1 << 20)]):
+        assert _orthogonalize(matrices=table, n=1 << 40, ws=0) == B.ERR_WORKSPACE
+    assert _orthogonalize(matrices=[(0, 10, 8, 20), (8, 2, 12, 15)], ws=0) == B.ERR_INVALID_ARG
