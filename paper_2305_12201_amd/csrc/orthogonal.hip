@@ -845,16 +845,14 @@ bool bounded(const double* coefficients, int steps)
         auto look = [&](double l, bool poly) {
             if (l > 0.0 && l < top) { if (poly) p = std::max(p, g(l)); else most = std::max(most, f(l)); }
         };
-        if (c != 0.0) {
-            const double disc = 9.0 * b * b - 20.0 * a * c;
-            if (disc >= 0.0) {
-                look((-3.0 * b + std::sqrt(disc)) / (10.0 * c), false);
-                look((-3.0 * b - std::sqrt(disc)) / (10.0 * c), false);
-            }
-            look(-b / (2.0 * c), true);
-        } else if (b != 0.0) {
-            look(-a / (3.0 * b), false);
+        // a + 3 b l + 5 c l^2 = 0; the sum that does not cancel gives one root, the product of both the other (also with c = 0)
+        const double disc = 9.0 * b * b - 20.0 * a * c;
+        if (disc >= 0.0) {
+            const double q = -0.5 * (3.0 * b + std::copysign(std::sqrt(disc), b));
+            if (c != 0.0) look(q / (5.0 * c), false);
+            if (q != 0.0) look(a / q, false);
         }
+        if (c != 0.0) look(-b / (2.0 * c), true);
         if (!(most <= MOST_X) || !(p <= MOST_P)) return false;
         u = most > 1e-3 ? most : 1e-3;
     }

@@ -159,3 +159,28 @@ def test_tables_of_different_strides_lie_apart():
     for table in ([(0, 10, 8, 20), (8, 1, 12, 12)], [(0, 10, 8, 20), (28, 4, 8, 40)], [(0, 1 << 20, 1, 1 << 19), (1, 1 << 18, 7, 1 << 20)]):
         assert _orthogonalize(matrices=table, n=1 << 40, ws=0) == B.ERR_WORKSPACE
     assert _orthogonalize(matrices=[(0, 10, 8, 20), (8, 2, 12, 15)], ws=0) == B.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("c", [0.0, 1e-17, -1e-17, 1e-12, -1e-9, 1e-300, 5e-324])
+def test_refuses_coefficients_by_their_largest_value_inside_the_range(c):
+    """11 s - 11 s^3 is 4.23 at s = 3^-1/2 and 0 at s = 1; 10 s - 10 s^3 is 3.85.  A fifth power that adds next to nothing changes
+    neither."""
+    assert _orthogonalize(steps=1, coefficients=[(11.0, -11.0, c)], ws=0) == B.ERR_INVALID_ARG
+    assert _orthogonalize(steps=1, coefficients=[(-11.0, 11.0, c)], ws=0) == B.ERR_INVALID_ARG
+    assert _orthogonalize(steps=1, coefficients=[(10.0, -10.0, c)], ws=0) == B.ERR_WORKSPACE
+
+
+def test_coefficients_against_values_on_a_grid():
+    """Every triple's largest values on a fine grid of [0, 1] decide, where they are not within 1e-3 of the limits."""
+    rng = np.random.default_rng(6)
+    s = np.linspace(0.0, 1.0, 20_001)
+    taken = 0
+    for _ in range(1500):
+        a, b, c = rng.normal(size=3) * 10.0 ** rng.uniform(-1, 1.3, 3)
+        most, poly = np.abs(a * s + b * s ** 3 + c * s ** 5).max(), np.abs(b * s ** 2 + c * s ** 4).max()
+        if abs(most - 3.9) < 4e-3 or abs(poly - 15.0) < 15e-3:
+            continue
+        ok = most < 3.9 and poly < 15.0
+        taken += ok
+        assert _orthogonalize(steps=1, coefficients=[(a, b, c)], ws=0) == (B.ERR_WORKSPACE if ok else B.ERR_INVALID_ARG), (a, b, c)
+    assert 100 < taken < 1400
