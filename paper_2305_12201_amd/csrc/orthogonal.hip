@@ -286,8 +286,8 @@ __global__ __launch_bounds__(256) void cut_kernel(Call p)
     double square = 0.0;
     for (uint32_t i = threadIdx.x; i < d.parts; i += 256) square += p.parts[d.part + i];
     square = sum_256(square, lds);
-    const double norm = sqrt(square) + p.eps;
-    const double inv = norm > 0.0 ? (double)SX / norm : (norm == 0.0 ? 0.0 : norm);
+    // (zeros stay zeros whatever eps is; the inverse of one below 10^-304 is infinite)
+    const double inv = square > 0.0 ? (double)SX / (sqrt(square) + p.eps) : square;
     const uint32_t local = blockIdx.x - d.cut;
     const int across = d.np / CUT;
     const int i0 = (int)(local / across) * CUT, j0 = (int)(local % across) * CUT;   // in X

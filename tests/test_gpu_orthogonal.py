@@ -555,3 +555,21 @@ def test_update_in_larger_tiles(sides, nesterov, dtype):
         bound = abs(step) * _gpu_tolerance(view(U, m), torch.float32) * torch.linalg.vector_norm(O) + \
             (HALF_STEP[dtype] + 3 * 2.0 ** -24) * torch.linalg.vector_norm(want.abs() + old.abs())
         assert err <= bound, (m, float(err), float(bound))
+
+
+@pytest.mark.parametrize("eps", [0.0, 5e-324, 1e-310, 1e-305, 1e-300, 1e300])
+def test_zeros_with_any_eps(eps):
+    x = torch.zeros(2 * 30 * 40, device="cuda")
+    x[30 * 40:] = _values(30, 40, "normal", 24).view(-1).cuda()
+    got = _orthogonalize(x, [(0, 30, 40), (30 * 40, 40, 30)], eps=eps).cpu()
+    assert torch.equal(got[:30 * 40], torch.zeros(30 * 40))
+    G = x[30 * 40:].cpu().view(40, 30)
+    want = _exact(G, eps=eps)
+    if eps < 1:
+        assert _error(got[30 * 40:].view(40, 30), want) <= _tolerance(G, torch.float32, eps=eps)
+    else:
+        assert torch.equal(got[30 * 40:], torch.zeros(30 * 40))     # below the smallest number
+    params = torch.ones(30 * 40, device="cuda")
+    zero = torch.zeros(30 * 40, device="cuda")
+    B.Orthogonalizer(30 * 40, [(0, 30, 40)], eps=eps).update(zero, zero.clone(), params, beta=0.9, alpha=-1.0)
+    assert (params == 1.0).all()
