@@ -509,7 +509,8 @@ def gravac_read_status(workspace, stream=None) -> dict:
 # --------------------------------------------------------------------------
 
 class Compressor:
-    """Owns the workspace and output buffers for repeated calls on one gradient shape."""
+    """Owns the workspace and output buffers for repeated calls on one gradient shape.  Calls on one object, and replays of
+    graphs that hold some, share them and must not overlap in time."""
 
     def __init__(self, n: int, cf_list, commit: int = 0, seg_offsets=None, device="cuda"):
         self.n = int(n)
@@ -545,15 +546,19 @@ class Compressor:
 
 
 class Orthogonalizer:
-    """Owns the workspace and the tables for repeated calls on the matrices of one flat vector."""
+    """Owns the workspace and the tables for repeated calls on the matrices of one flat vector.
+
+    The one workspace is every call's, the captured ones' too: calls on one object, and replays of graphs that hold some, must
+    follow one another on one stream or be ordered by events.  Calls that may overlap in time take an object each."""
 
     def __init__(self, n: int, matrices, dtype=torch.float32, steps: int = 5, coefficients=None, eps: float = 1e-7,
                  device="cuda"):
         self.n = int(n)
-        self.matrices = _matrices(matrices)
+        self.matrices = _matrices(matrices).copy()         # (the caller's arrays may change)
         self.dtype = dtype
         self.steps = int(steps)
-        self.coefficients = _coefficients(coefficients, self.steps)
+        c = _coefficients(coefficients, self.steps)
+        self.coefficients = None if c is None else c.copy()
         self.eps = float(eps)
         self.workspace = torch.empty(gravac_orthogonalize_workspace_bytes(self.matrices, dtype), dtype=torch.uint8,
                                      device=device)

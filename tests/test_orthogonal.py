@@ -184,3 +184,13 @@ def test_coefficients_against_values_on_a_grid():
         taken += ok
         assert _orthogonalize(steps=1, coefficients=[(a, b, c)], ws=0) == (B.ERR_WORKSPACE if ok else B.ERR_INVALID_ARG), (a, b, c)
     assert 100 < taken < 1400
+
+
+def test_an_orthogonalizer_keeps_its_tables():
+    table, each = np.array(TABLE, dtype=np.int64), np.array([(1.0, 0.0, 0.0), (1.5, -0.5, 0.0)])
+    o = B.Orthogonalizer(1000, table, steps=2, coefficients=each, device="cpu")
+    before = o.matrices.tolist(), o.coefficients.tolist(), o.workspace.numel()
+    table[:, 1] *= 2
+    each[:] = 7.0
+    assert (o.matrices.tolist(), o.coefficients.tolist()) == before[:2]
+    assert B.gravac_orthogonalize_workspace_bytes(o.matrices) == before[2]
