@@ -341,8 +341,9 @@ __device__ __forceinline__ S uniform(S x)
 enum Product { GRAM, POLY, NEXT, LAST };   // A; P; X of the next step; X of the last one, into the caller's buffers
 
 // Sixteen rows of a slab from global memory into LDS without a register in between, 16 bytes per lane; AT is added to both
-// addresses.  The LDS address is the wavefront's.  The compiler does not count these loads (arrived() does), and nothing
-// else in the kernel uses M0.
+// addresses.  The LDS address is the wavefront's.  The compiler does not count these loads (arrived() does).  M0 is among the
+// registers that it keeps for itself, so it takes no clobber of it: it writes M0 right before those of its own instructions that
+// read it, of which there are none here (the kernels' assembly names M0 in this statement alone).
 template <int AT>
 __device__ __forceinline__ void fetch_16(const char* base, uint32_t offset, uint32_t lds)
 {
