@@ -384,7 +384,7 @@ int gravac_embedding_gradient(const void* grad_out, int grad_type, int64_t n_tok
  *   type            GRAVAC_FLOAT32, GRAVAC_BFLOAT16 or GRAVAC_FLOAT16: elements of in and out, or of the parameters.  The
  *                   products are as exact as in binary32 with all of them; a 16-bit result is rounded once, at the end.
  *                   More exactly, an entry of X is held to 2^-22 of itself or to 2^-39 of X's norm before the first step,
- *                   whichever is more, and one of X X^T and of its polynomial to 2^-22 or 2^-37.  Up to ten steps of the
+ *                   whichever is more, and one of X X^T and of its polynomial to 2^-22 or 2^-37.  Up to eight steps of the
  *                   default coefficients that is no more than what binary32 loses.  With more of them, rows and columns
  *                   below 10^-5 of the others are raised with a relative error of about 2 * 10^-11 over their share of the
  *                   matrix's norm: one of 10^-6 to four digits, one of 10^-8 to two.

@@ -8,7 +8,7 @@
 // written by one wavefront.
 //
 // Measured: the lookup of 65,539 rows of 8 KiB 136 us (5.1 TB/s; a copy of 2 GiB runs at 4.9); the gradient of 131,072
-// tokens on as many rows of 4096 719 us (4.5 TB/s), of 700 tokens on 33,278 rows of 650 16.6 us (5.2 TB/s, nearly all of
+// tokens on as many rows of 4096 720 us (4.5 TB/s), of 700 tokens on 33,278 rows of 650 16 to 18 us (4.9 to 5.5 TB/s, nearly all of
 // it zeros).  Calls of a few tokens are bound by the launch, 7 us with the call itself.
 
 #include <hip/hip_runtime.h>
@@ -316,8 +316,8 @@ __global__ __launch_bounds__(SORT_T) void count_kernel(GradParams p, int from, i
 }
 
 // ... and the tokens moved to their places: behind all smaller digits, and behind the same digit of earlier workgroups.
-// (Workgroups that count all tokens themselves spare a launch per pass and take as long: 16,381 tokens 15.3 us instead of
-// 8.1 and 3 to 5 for the counts.)
+// (Workgroups that count all tokens themselves spare a launch per pass and took as long: 16,381 tokens in tiles of four tokens per
+// thread 15.3 us instead of 8.1 and 3 to 5 for the counts.  With tiles of one the two kernels take 6.0 and 4.6.)
 template <int ROUNDS>
 __global__ __launch_bounds__(SORT_T) void scatter_kernel(GradParams p, int from, int to, int shift)
 {
@@ -595,8 +595,8 @@ __global__ __launch_bounds__(64 * JOIN_W) void join_kernel(GradParams p, int sor
 
 // At most FEW tokens, one launch: a workgroup per token (and 64 * N columns) looks at all of them; the first of its kind adds
 // up the rows of all of its kind, its wavefronts in turn, and their sums in order.  The first workgroups clear the rows
-// that no token names.  (700 tokens of 33,278 rows of 650: 16 us, 32 with a sort beside the
-// clearing and two more launches.)
+// that no token names.  (700 tokens of 33,278 rows of 650: 16 to 18 us, 32 with a sort beside the clearing and two more
+// launches.)
 template <typename E, bool ADD, int N>
 __global__ __launch_bounds__(FEW_T) void sum_few_kernel(GradParams p)
 {

@@ -17,17 +17,17 @@
 // and X is stored times 2^14, E and Q times 2^12, so that the largest entries possible, which the host bounds, lie just below 65504.
 // Of an entry of X below 2^-17 (one of E or Q below 2^-15) the lower part is a subnormal number of binary16: it is off by 2^-39 (2^-37)
 // at most, no longer by 2^-22 of itself, and the steps that raise it raise that too.  (Powers of two that follow the matrix's size,
-// with typical entries near 1, leave less: a 16 x 64 matrix with one row 10^5 times the others was off by 5.7e-4 after 16 steps, so
-// by 2e-6.)
+// with typical entries near 1, leave less: a 16 x 64 matrix with one row 10^5 times the others was off by 5.2e-4 after 10 steps
+// and is by 1.0e-6.)
 //
 // Memory.  Every product is of the form C = L R^T with rows of L and R contiguous along the sum: X is kept as X and as X^T,
 // both written by the product that makes them.  Rows and columns are padded with zeros to whole tiles, so the products have
-// no edges; their sums end with the matrix (four 2600 x 650 in float32: 511 -> 473 us).
+// no edges; their sums end with the matrix (four 2600 x 650 in float32 took 511 us with sums over the padding, and 473).
 //
-// Measured, five steps: 4096 x 4096 in bfloat16 3.82 ms (three products each: 1080 TFLOP/s of matrix instructions; the clock gives way
-// to power there: 1.7 GHz), the 16 matrices of the VGG16 shape in float32 21.8 to 22.4 ms (1130 TFLOP/s), the 105 of ResNet101 1.83
-// to 1.87 ms, where X, of 178 MB, passes memory four times a step, 512 x 128 in bfloat16 93 us, 15 products one after the other at 4 to
-// 6 us.
+// Measured, five steps, three products each: 4096 x 4096 in bfloat16 3.7 to 4.0 ms (1020 to 1110 TFLOP/s of matrix instructions; the
+// clock gives way to power there: 1.7 GHz), the 16 matrices of the VGG16 shape in float32 21.8 to 22.4 ms (1100 to 1130), the 105 of
+// ResNet101 1.74 to 1.87 ms, where X, of 178 MB, passes memory four times a step, 512 x 128 in bfloat16 93 us, 15 products one after
+// the other at 4.6 to 6.5 us.
 
 #include <hip/hip_runtime.h>
 
@@ -689,9 +689,10 @@ int64_t large_side(const int64_t* matrix) { return std::max(matrix[1], matrix[2]
 
 // Side of the products' tiles.  Tiles of 256 need half the LDS traffic, but there are a quarter as many and more of them is
 // padding: they pay where A has tiles for half of the compute units, from matrices of four or more a side that are most of the
-// work.  Measured in us with tiles of 128 and of 256, five steps, sums over the padding too: 2560 x 5120 1857 and 2831 (55 tiles of A), twelve
-// 1024 x 1024 999 and 1214 (120), four 2048 x 2048 2269 and 2318 (144), 4096 x 4096 4119 and 4064 (136), twelve 1500 x 3000 4881 and
-// 4722 (252).
+// work.  Measured in us with tiles of 128 and of 256, five steps in float32: 2560 x 5120 1899 and 2796 (55 tiles of A), twelve
+// 1024 x 1024 998 and 1205 (120), four 2048 x 2048 2311 and 2314 (144), 4096 x 4096 4196 and 4039 (136), twelve 1500 x 3000 4765 and
+// 4639 (252), twenty-four 1024 x 4096 5874 and 5443 (240), three 4096 x 11008 26.2 and 23.7 ms (408).  It is blind to sides just
+// beyond a multiple of 256, whose padding makes it lose: nine 1025 x 2100 1590 and 2114 (135).
 int tile_of(const int64_t* matrices, int n_mat)
 {
     double all = 0.0, large = 0.0, tiles = 0.0;
@@ -715,11 +716,14 @@ uint64_t tiles_of(const int64_t* matrix, int k, int64_t side, int64_t pad)
 }
 
 // Tiles of 64 where those of 128 would be few: they bring more compute units to work and their epilogues are short.  us for five
-// steps in float32, sums over the padding too, with A, P and X in tiles of 128 / A in 64 / A and P / all: 512 x 512 234, 202, 165, 135; 1024 x 1024 344,
-// 297, 241, 197; four 2600 x 650 (84 tiles of 128 of A and P, 504 of X) 548, 492, 465, 542; 1536 x 1536 (78, 144) 464, 438, 398,
-// 418; four 1024 x 1024 (144, 256) 427, 439, 438, 469; the ResNet101 shape (405, 2700) with P alone in 64 1924 -> 1863.
-// Twelve 300 x 900 are 245 with X in 128 and 228 in 64 for the padding alone.
-// P among tiles of 256 takes 128 where a last round of those would leave more units idle: VGG16 shape 22.6 -> 21.9 ms.
+// steps in float32 with A, P and X in tiles of 128 / A in 64 / A and P / all: 512 x 512 233, 201, 163, 132; 1024 x 1024 341, 293,
+// 236, 196; four 2600 x 650 (84 tiles of 128 of A and P, 504 of X) 587, 520, 493, 510; 1536 x 1536 (78, 144) 465, 443, 405, 433;
+// 2048 x 2048 (136, 256) 712, 736, 754, 811; four 1024 x 1024 (144, 256) 450, 457, 460, 492.  P alone in 64: 465 -> 437 with 78 tiles,
+// 782 -> 778 with 288 (eight 1024 x 1024), 1740 -> 1742 with 405 (the ResNet101 shape), 960 -> 1004 with 504 (twenty-four 768 x 768).
+// Twelve 300 x 900 are 258 with X in 128 and 217 in 64 for the padding.
+// P among tiles of 256 takes 128 where a last round of those would leave more units idle: VGG16 shape 22.5 -> 21.9 ms, sixteen
+// 2048 x 2048 8.27 -> 8.06, nine 1025 x 2100 2.11 -> 1.96.  (0.93: where
+// all units are busy either way, tiles of 128 are 3 to 10 % slower, as the figures above say.)
 void choose_sides(const int64_t* matrices, int n_mat, Layout& L)
 {
     const int tile = tile_of(matrices, n_mat);
