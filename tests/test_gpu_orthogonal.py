@@ -573,3 +573,29 @@ def test_zeros_with_any_eps(eps):
     zero = torch.zeros(30 * 40, device="cuda")
     B.Orthogonalizer(30 * 40, [(0, 30, 40)], eps=eps).update(zero, zero.clone(), params, beta=0.9, alpha=-1.0)
     assert (params == 1.0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_largest_entries_that_the_coefficients_allow(dtype):
+    """Singular values up to 3.89 in single entries, and the products of them: no operand leaves its range."""
+    top = 3.89
+    each = [(top, 0.0, 0.0), tuple(top * k / top ** e for k, e in ((5, 1), (-20, 3), (16, 5))), (1.0, 0.0, 0.0),
+            tuple(top * k / top ** e for k, e in ((5, 1), (-20, 3), (16, 5)))]       # the fifth Chebyshev polynomial on [-top, top]
+
+    def exact(G, t):
+        X = G.to(t)
+        X = X / (torch.linalg.vector_norm(G.double()).to(t) + 1e-7)
+        for a, b, c in each:
+            A = X @ X.t()
+            X = a * X + (b * A + c * (A @ A)) @ X
+        return X
+
+    for G in (torch.ones(1, 1), -torch.ones(1, 1), torch.diag(torch.tensor([1.0, 0.0])), torch.ones(40, 70), torch.diag(torch.tensor([1.0, 0.5, 1e-3])),
+              torch.tensor([[1.0, 1.0], [-1.0, 1.0]]), torch.outer(torch.eye(130)[5], torch.ones(300)), _values(64, 200, "low rank", 25)):
+        G = G.to(dtype)
+        got = _orthogonalize(G.cuda().view(-1), [(0, *G.shape)], steps=4, coefficients=each).cpu().view(G.shape)
+        want = exact(G, torch.float64)
+        diff = got.double() - want if dtype == torch.float32 else _beyond_rounding(got, want)
+        bound = 12 * _error(exact(G, torch.float32), want) + 25 * 25 * top * 2.0 ** -22    # (slopes of 25 top / top at the ends)
+        assert torch.isfinite(got).all()
+        assert torch.linalg.vector_norm(diff) <= bound * torch.linalg.vector_norm(want), G.shape
