@@ -722,8 +722,8 @@ uint64_t tiles_of(const int64_t* matrix, int k, int64_t side, int64_t pad)
 // 782 -> 778 with 288 (eight 1024 x 1024), 1740 -> 1742 with 405 (the ResNet101 shape), 960 -> 1004 with 504 (twenty-four 768 x 768).
 // Twelve 300 x 900 are 258 with X in 128 and 217 in 64 for the padding.
 // P among tiles of 256 takes 128 where a last round of those would leave more units idle: VGG16 shape 22.5 -> 21.9 ms, sixteen
-// 2048 x 2048 8.27 -> 8.06, nine 1025 x 2100 2.11 -> 1.96.  (0.93: where
-// all units are busy either way, tiles of 128 are 3 to 10 % slower, as the figures above say.)
+// 2048 x 2048 8.27 -> 8.06, nine 1025 x 2100 2.11 -> 1.96.  (0.93: where all units are busy either way,
+// tiles of 128 are 3 to 10 % slower, as the figures above say.)
 void choose_sides(const int64_t* matrices, int n_mat, Layout& L)
 {
     const int tile = tile_of(matrices, n_mat);
